@@ -15,7 +15,8 @@ ROOT = PKG.parent
 CSRC = PKG / "csrc"
 INCLUDE = ROOT / "include"
 LIB_PATH = PKG / "libspconv.so"
-SOURCES = [CSRC / "spconv.hip", CSRC / "dense.hip", CSRC / "matrix.hip", CSRC / "pack.cpp"]
+SOURCES = [CSRC / "spconv.hip", CSRC / "dense.hip", CSRC / "matrix.hip", CSRC / "pack.cpp", CSRC / "cache.hip",
+           CSRC / "blocks.hip", CSRC / "attention.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 

@@ -1,0 +1,486 @@
+// Attention over listed blocks (spconv_block_attention).
+//
+// For a query q and the keys S that its row lists and its position lets it see:
+//   out = sum_S exp(x_j - m) v_j / sum_S exp(x_j - m),  x_j = scale * q.k_j, m = max_S x_j,
+// in one pass over the keys: when a tile raises the running maximum from m to m',
+// sum and output so far are multiplied by exp(m - m'). Everything is held in powers of two
+// (x in units of ln 2), in fp32.
+//
+// Matrix tiles are formed transposed: S^T = K Q^T has queries as columns, so that a lane
+// holds weights of one query only, its maximum and sum are a lane's own numbers, and the
+// weights are already where the second product O^T = V^T P^T wants its right
+// operand: the order of the keys inside a product is free, so V^T's rows are read in the order
+// in which the weights came out (slot 8*(l/16) + 4*t + i of lane l is key 16*t + 4*(l/16) + i).
+#include "batch.h"
+
+namespace {
+
+constexpr float kInf = __builtin_huge_valf();
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLn2 = 0.69314718055994530942f;
+
+template <typename T>
+struct Frag8 {
+    typedef T type __attribute__((ext_vector_type(8)));
+};
+
+template <typename T>
+using frag_t = typename Frag8<T>::type;
+
+// acc += A B for 16x16 tiles, 32 deep: eight elements of a row of A and of a column of B per lane.
+__device__ __forceinline__ f32x4 mma(frag_t<__bf16> a, frag_t<__bf16> b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mma(frag_t<_Float16> a, frag_t<_Float16> b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mma(frag_t<float> a, frag_t<float> b, f32x4 c) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], c, 0, 0, 0);
+    return c;
+}
+
+template <typename T>
+__device__ __forceinline__ frag_t<T> zero_frag() {
+    frag_t<T> z;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) z[i] = (T)0.0f;
+    return z;
+}
+
+// Max and sum over the four lanes that hold one column (lanes l, l+16, l+32, l+48).
+__device__ __forceinline__ float column_max(float x) {
+    const uint32_t u = __float_as_uint(x);
+    const auto a = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    const float y = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const uint32_t w = __float_as_uint(y);
+    const auto b = __builtin_amdgcn_permlane16_swap(w, w, false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
+__device__ __forceinline__ float column_sum(float x) {
+    const uint32_t u = __float_as_uint(x);
+    const auto a = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    const float y = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    const uint32_t w = __float_as_uint(y);
+    const auto b = __builtin_amdgcn_permlane16_swap(w, w, false, false);
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+struct AttnArgs {
+    spconv_batch B;
+    const void *q;
+    int64_t q_token, q_head;
+    const void *k_cache, *v_cache;
+    const int32_t *blocks, *counts;
+    void *out;
+    int64_t o_token, o_head;
+    float *lse;
+    float *part, *stat;  // workspace: [item][split][16][dim], [item][split][16][2]
+    int64_t items;       // rows * heads * tiles
+    int heads, group, dim, keep, tiles, splits, q_aligned;
+    float scale2;  // scale / ln 2
+    Div tile_div, head_div, group_div, split_div, slab_div;
+};
+
+// The 16 (token, head) pairs of a tile of a row, token by token: pair m is token m / group, head m % group.
+struct Pairs {
+    Row r;
+    int h, m0, last;  // last: position of the tile's last token, -1 if it has none
+    int64_t rh;
+};
+
+__device__ __forceinline__ Pairs find_pairs(const AttnArgs &a, uint32_t item) {
+    Pairs p;
+    const uint32_t rh = item / a.tile_div;
+    p.m0 = (int)(item - rh * a.tile_div.d) * 16;
+    const int row = (int)(rh / a.head_div);
+    p.h = (int)(rh - row * a.head_div.d);
+    p.rh = rh;
+    p.r = find_row(a.B, row);
+    const int end = min(p.r.n * a.group, p.m0 + 16);
+    p.last = end > p.m0 ? p.r.p0 + (int)((uint32_t)(end - 1) / a.group_div) : -1;
+    if (end <= p.m0) p.r.n = 0;
+    return p;
+}
+
+// Output and log-sum-exp of a sum of weights relative to 2^ref; 0 and -infinity of an empty one.
+__device__ __forceinline__ float weighted(float acc, float sum) { return sum == 0.0f ? 0.0f : acc / sum; }
+__device__ __forceinline__ float log_sum(float ref, float sum) {
+    return sum == 0.0f ? -kInf : (ref + __builtin_amdgcn_logf(sum)) * kLn2;
+}
+
+constexpr int kEntries = 256;  // list entries whose pages are looked up at a time
+
+__device__ __forceinline__ bool not_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u; }
+
+// One workgroup a (row, head, 16 pairs, share of the row's keys). Its four waves take 32
+// keys in turn, each with a running maximum, sum and output of its own, joined
+// at the end; shares of a row (splits) are joined by join_kernel.
+template <typename T, int NK>
+__global__ __launch_bounds__(256) void rows_kernel(AttnArgs a) {
+    constexpr int DP = NK * 32, W = kPer16<T>, UPR = DP / W;  // 16-byte units of a row
+    constexpr int NU = 16 * UPR / 64;                         // units a lane holds of 16 rows
+    constexpr int kTile = 32 * DP * (int)sizeof(T);
+    constexpr int kJoin = 16 * (DP + 4) * 4;
+    constexpr int kPerWave = kTile > kJoin ? kTile : kJoin;
+    __shared__ __attribute__((aligned(16))) char lds[4 * kPerWave];
+    __shared__ int e_block[kEntries], e_page[kEntries];
+    __shared__ float w_max[4][16], w_sum[4][16];
+    typedef typename VecOf<T, W>::type V;
+
+    const int64_t idx = grid_index();
+    if (idx >= a.items * a.splits) return;
+    const uint32_t item = (uint32_t)idx / a.split_div;
+    const int split = (int)((uint32_t)idx - item * a.split_div.d);
+    const Pairs P = find_pairs(a, item);
+    if (P.r.n == 0) return;
+    const spconv_batch &B = a.B;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, part = lane >> 4;
+    const int D = a.dim, spb = B.block >> 4;
+
+    // Query of this lane's column.
+    const int m = P.m0 + col, tok = (uint32_t)m / a.group_div;
+    const int pos = tok < P.r.n ? P.r.p0 + tok : -1;
+    frag_t<T> q[NK];
+    {
+        const T *src = (const T *)a.q + (int64_t)(P.r.t0 + tok) * a.q_token +
+                       (int64_t)(P.h * a.group + (m - tok * a.group)) * a.q_head;
+#pragma unroll
+        for (int k = 0; k < NK; ++k) {
+            const int d = k * 32 + part * 8;
+            q[k] = zero_frag<T>();
+            if (tok < P.r.n && d < D) {
+                if (a.q_aligned) {
+                    q[k] = *reinterpret_cast<const frag_t<T> *>(src + d);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) q[k][i] = src[d + i];
+                }
+            }
+        }
+    }
+
+    // This share of the row's slabs (16 keys of a block).
+    int entries = 0;
+    if (P.last >= 0) entries = min(P.last / B.block + 1, B.max_blocks);
+    if (a.blocks) entries = P.last < 0 ? 0 : a.counts ? clamp_int(a.counts[P.rh], 0, a.keep) : a.keep;
+    const int64_t slabs = (int64_t)entries * spb;
+    const int64_t per = ((slabs + 1) / 2 + a.splits - 1) / a.splits * 2;
+    const int64_t s_lo = min(per * split, slabs), s_hi = min(s_lo + per, slabs);
+    const int first_pos = P.r.p0 + (int)((uint32_t)P.m0 / a.group_div);  // position of the tile's first token
+
+    constexpr int NT = DP / 16;
+    f32x4 o[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) o[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    float top = -kInf, sum = 0.0f;
+    T *vt = reinterpret_cast<T *>(lds + wave * kPerWave);
+
+    for (int e0 = s_lo < s_hi ? (int)(s_lo / spb) : 0; (int64_t)e0 * spb < s_hi; e0 += kEntries) {
+        __syncthreads();
+        {
+            const int e = e0 + tid;
+            int j = -1, page = -1;
+            if (e < entries) {
+                j = a.blocks ? a.blocks[P.rh * a.keep + e] : e;
+                if (j >= 0 && j <= P.last / B.block && j < B.max_blocks) page = page_of(B, P.r.b, j);
+            }
+            e_block[tid] = j;
+            e_page[tid] = page;
+        }
+        __syncthreads();
+        const int lo = (int)(max(s_lo, (int64_t)e0 * spb) - (int64_t)e0 * spb);
+        const int hi = (int)(min(s_hi, ((int64_t)e0 + kEntries) * spb) - (int64_t)e0 * spb);
+        for (int s = lo + 2 * wave; s < hi; s += 8) {
+            int key0[2];
+            int64_t base[2];
+            bool there[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const int e = (uint32_t)(s + t) / a.slab_div, sub = (s + t) - e * spb;
+                there[t] = false;
+                key0[t] = 0;
+                base[t] = 0;
+                if (s + t < hi) {
+                    const int page = __builtin_amdgcn_readfirstlane(e_page[e]);
+                    key0[t] = __builtin_amdgcn_readfirstlane(e_block[e]) * B.block + sub * 16;
+                    there[t] = page >= 0 && key0[t] <= P.last;
+                    base[t] = (((int64_t)page * a.heads + P.h) * B.block + sub * 16) * D;
+                }
+            }
+            if (!there[0] && !there[1]) continue;
+            // Keys: rows of the first product straight from memory.
+            f32x4 x[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                x[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                if (there[t]) {
+                    const T *src = (const T *)a.k_cache + base[t] + col * D + part * 8;
+#pragma unroll
+                    for (int k = 0; k < NK; ++k) {
+                        frag_t<T> f = zero_frag<T>();
+                        if (k * 32 + part * 8 < D) f = *reinterpret_cast<const frag_t<T> *>(src + k * 32);
+                        x[t] = mma(f, q[k], x[t]);
+                    }
+                }
+            }
+            // Values: to LDS by rows. Rows that no query of the tile sees are zero, whatever
+            // lies there: their weights are zero too, and zero times infinity is not.
+            bool odd = false;  // a value that is not finite
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const bool mixed = there[t] && key0[t] + 15 > first_pos;
+#pragma unroll
+                for (int i = 0; i < NU; ++i) {
+                    const int u = i * 64 + lane, row = u / UPR, c = u % UPR;
+                    V v;
+#pragma unroll
+                    for (int e = 0; e < W; ++e) v[e] = (T)0.0f;
+                    if (there[t] && key0[t] + row <= P.last && c * W < D)
+                        v = *reinterpret_cast<const V *>((const T *)a.v_cache + base[t] + row * D + c * W);
+                    if (mixed) {
+#pragma unroll
+                        for (int e = 0; e < W; ++e)
+                            if (not_finite((float)v[e])) {
+                                odd = true;
+                                v[e] = (T)0.0f;
+                            }
+                    }
+                    const int lr = t * 16 + row;
+                    const int sw = sizeof(T) == 2 ? (lr & (UPR - 1)) : (((lr >> 2) & 3) << 2);
+                    *reinterpret_cast<V *>(vt + lr * DP + (c ^ sw) * W) = v;
+                }
+            }
+            // Weights.
+            float hi8 = -kInf;
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const bool seen = there[t] && key0[t] + part * 4 + i <= pos;
+                    x[t][i] = seen ? x[t][i] * a.scale2 : -kInf;
+                    hi8 = fmaxf(hi8, x[t][i]);
+                }
+            const float next = fmaxf(top, column_max(hi8));
+            const float ref = next == -kInf ? 0.0f : next;
+            const float shrink = __builtin_amdgcn_exp2f(top - ref);
+            top = next;
+            frag_t<T> w;
+            float p[8], total = 0.0f;
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    p[t * 4 + i] = __builtin_amdgcn_exp2f(x[t][i] - ref);
+                    total += p[t * 4 + i];
+                    w[t * 4 + i] = (T)p[t * 4 + i];
+                }
+            sum = sum * shrink + total;
+            if (__ballot(shrink != 1.0f)) {
+#pragma unroll
+                for (int t = 0; t < NT; ++t) o[t] *= shrink;
+            }
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                if (t * 16 >= D) break;
+                frag_t<T> f;
+                if constexpr (sizeof(T) == 2) {
+                    typedef short s16x4 __attribute__((ext_vector_type(4)));
+                    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+                    union {
+                        s16x4 h[2];
+                        frag_t<T> f;
+                    } u;
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) {
+                        const int lr = b * 16 + part * 4 + (col >> 2);
+                        const int c = t * 2 + ((col & 3) >> 1);
+                        T *src = vt + lr * DP + ((c ^ (lr & (UPR - 1))) * W) + (col & 1) * 4;
+                        u.h[b] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)src);
+                    }
+                    f = u.f;
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int lr = (i >> 2) * 16 + part * 4 + (i & 3), d = t * 16 + col;
+                        f[i] = vt[lr * DP + (((d >> 2) ^ (((lr >> 2) & 3) << 2)) << 2) + (d & 3)];
+                    }
+                }
+                o[t] = mma(f, w, o[t]);
+            }
+            if (__ballot(odd)) {
+                // Values that are not finite, in a tile of which some queries see a part only: one by one.
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    if (!there[t] || key0[t] + 15 <= first_pos) continue;
+                    for (int kr = 0; kr < 16; ++kr) {
+                        const float p0 = p[t * 4], p1 = p[t * 4 + 1], p2 = p[t * 4 + 2], p3 = p[t * 4 + 3];
+                        const float mine = (kr & 3) == 0 ? p0 : (kr & 3) == 1 ? p1 : (kr & 3) == 2 ? p2 : p3;
+                        const float weight = __shfl(mine, (kr >> 2) * 16 + col);
+                        if (key0[t] + kr > pos) continue;
+                        const T *src = (const T *)a.v_cache + base[t] + kr * D;
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const int d = n * 16 + part * 4 + i;
+                                if (d >= D) continue;
+                                const float v = (float)src[d];
+                                if (not_finite(v)) o[n][i] += weight * v;
+                            }
+                    }
+                }
+            }
+            __builtin_amdgcn_wave_barrier();
+        }
+    }
+    sum = column_sum(sum);
+
+    // Join the waves.
+    __syncthreads();
+    float *mine = reinterpret_cast<float *>(lds + wave * kPerWave);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) *reinterpret_cast<f32x4 *>(mine + col * (DP + 4) + t * 16 + part * 4) = o[t];
+    if (part == 0) {
+        w_max[wave][col] = top;
+        w_sum[wave][col] = sum;
+    }
+    __syncthreads();
+    const int pairs = min(16, P.r.n * a.group - P.m0);
+    for (int i = tid; i < pairs * DP; i += 256) {
+        const int c = i / DP, d = i % DP;
+        if (d >= D) continue;
+        float mx = -kInf;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) mx = fmaxf(mx, w_max[w][c]);
+        const float ref = mx == -kInf ? 0.0f : mx;
+        float acc = 0.0f, l = 0.0f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float f = __builtin_amdgcn_exp2f(w_max[w][c] - ref);
+            l += f * w_sum[w][c];
+            acc += f * reinterpret_cast<const float *>(lds + w * kPerWave)[c * (DP + 4) + d];
+        }
+        if (a.splits == 1) {
+            const int mm = P.m0 + c, tk = (uint32_t)mm / a.group_div, g = P.h * a.group + (mm - tk * a.group);
+            ((T *)a.out)[(int64_t)(P.r.t0 + tk) * a.o_token + (int64_t)g * a.o_head + d] = (T)weighted(acc, l);
+            if (a.lse && d == 0) a.lse[(int64_t)(P.r.t0 + tk) * (a.heads * a.group) + g] = log_sum(ref, l);
+        } else {
+            const int64_t at = ((int64_t)item * a.splits + split) * 16 + c;
+            a.part[at * D + d] = acc;
+            if (d == 0) {
+                a.stat[at * 2] = mx;
+                a.stat[at * 2 + 1] = l;
+            }
+        }
+    }
+}
+
+// Joins the shares of a pair: one workgroup a (row, head, tile, pair).
+template <typename T>
+__global__ __launch_bounds__(256) void join_kernel(AttnArgs a) {
+    const int64_t idx = grid_index();
+    if (idx >= a.items * 16) return;
+    const uint32_t item = (uint32_t)(idx >> 4);
+    const int c = (int)(idx & 15);
+    const Pairs P = find_pairs(a, item);
+    if (P.r.n == 0 || P.m0 + c >= P.r.n * a.group) return;
+    const float *stat = a.stat + ((int64_t)item * a.splits * 16 + c) * 2;
+    const float *part = a.part + ((int64_t)item * a.splits * 16 + c) * a.dim;
+    float mx = -kInf;
+    for (int s = 0; s < a.splits; ++s) mx = fmaxf(mx, stat[s * 32]);
+    const int m = P.m0 + c, tok = (uint32_t)m / a.group_div, g = P.h * a.group + (m - tok * a.group);
+    const int d = threadIdx.x;
+    if (d >= a.dim) return;
+    const float ref = mx == -kInf ? 0.0f : mx;
+    float acc = 0.0f, l = 0.0f;
+    for (int s = 0; s < a.splits; ++s) {
+        const float x = stat[s * 32], y = stat[s * 32 + 1];
+        if (x == -kInf && y == 0.0f) continue;
+        const float f = __builtin_amdgcn_exp2f(x - ref);
+        l += f * y;
+        acc += f * part[(int64_t)s * 16 * a.dim + d];
+    }
+    ((T *)a.out)[(int64_t)(P.r.t0 + tok) * a.o_token + (int64_t)g * a.o_head + d] = (T)weighted(acc, l);
+    if (a.lse && d == 0) a.lse[(int64_t)(P.r.t0 + tok) * (a.heads * a.group) + g] = log_sum(ref, l);
+}
+
+struct Plan {
+    int64_t items;
+    int tiles, splits;
+    int64_t part_bytes, bytes;
+};
+
+// False for sizes out of range.
+bool plan_of(const spconv_batch *B, int q_heads, int heads, int dim, int keep, Plan *p) {
+    const int group = q_heads / heads;
+    p->tiles = (B->q_block * group + 15) / 16;
+    p->items = rows_of(B) * heads * p->tiles;
+    if (p->items >= ((int64_t)1 << 27)) return false;
+    // Shares of a row's keys: enough workgroups for two on every CU, 256 keys (two turns of the waves) each at least.
+    const int64_t keys = (int64_t)(keep ? keep : B->max_blocks) * B->block;
+    int64_t splits = (512 + p->items - 1) / p->items;
+    splits = std::min<int64_t>(splits, (keys + 255) / 256);
+    p->splits = (int)std::max<int64_t>(1, splits);
+    p->part_bytes = p->bytes = 0;
+    if (p->splits > 1) {
+        p->part_bytes = p->items * p->splits * 16 * dim * 4;
+        p->bytes = p->part_bytes + p->items * p->splits * 16 * 2 * 4;
+    }
+    return true;
+}
+
+template <typename T>
+int attention_of(const AttnArgs &a, hipStream_t stream) {
+    const dim3 grid = grid_of(a.items * a.splits);
+    if (a.dim <= 64)
+        rows_kernel<T, 2><<<grid, 256, 0, stream>>>(a);
+    else if (a.dim <= 128)
+        rows_kernel<T, 4><<<grid, 256, 0, stream>>>(a);
+    else
+        rows_kernel<T, 8><<<grid, 256, 0, stream>>>(a);
+    if (hipGetLastError() != hipSuccess) return SPCONV_EHIP;
+    if (a.splits > 1) {
+        join_kernel<T><<<grid_of(a.items * 16), 256, 0, stream>>>(a);
+        return launched();
+    }
+    return SPCONV_OK;
+}
+
+}  // namespace
+
+extern "C" int spconv_attention_workspace(int dtype, const spconv_batch *batch, int q_heads, int heads, int dim, int keep,
+                                          int64_t *bytes) {
+    Plan p;
+    if (!batch_ok(batch) || !dtype_ok(dtype) || !heads_ok(q_heads, heads, dim) || keep < 0 || bytes == nullptr ||
+        !plan_of(batch, q_heads, heads, dim, keep, &p))
+        return SPCONV_EINVAL;
+    *bytes = p.bytes;
+    return SPCONV_OK;
+}
+
+extern "C" int spconv_block_attention(int dtype, const spconv_batch *batch, const void *q, int64_t q_token,
+                                      int64_t q_head, int q_heads, int heads, int dim, const void *k_cache,
+                                      const void *v_cache, float scale, const int32_t *blocks, const int32_t *counts,
+                                      int keep, void *out, int64_t out_token, int64_t out_head, float *lse,
+                                      void *workspace, int64_t workspace_bytes, hipStream_t stream) {
+    Plan p;
+    if (!batch_ok(batch) || !batch_arrays_ok(batch) || !dtype_ok(dtype) || !heads_ok(q_heads, heads, dim) ||
+        q == nullptr || k_cache == nullptr || v_cache == nullptr || out == nullptr || q_token < 0 || q_head < 0 ||
+        !out_strides_ok(batch->tokens, q_heads, dim, out_token, out_head) || !aligned16(k_cache) ||
+        !aligned16(v_cache) || !std::isfinite(scale) || keep < 0 || (blocks == nullptr) != (keep == 0) ||
+        (counts != nullptr && blocks == nullptr) || !plan_of(batch, q_heads, heads, dim, keep, &p))
+        return SPCONV_EINVAL;
+    if (p.bytes > 0 && (workspace == nullptr || !aligned16(workspace) || workspace_bytes < p.bytes)) return SPCONV_EINVAL;
+    AttnArgs a{*batch, q, q_token, q_head, k_cache, v_cache, blocks, counts, out, out_token, out_head, lse,
+               (float *)workspace, nullptr, p.items, heads, q_heads / heads, dim, keep, p.tiles, p.splits,
+               rows_aligned16(q, q_token, q_head, size_of(dtype)), scale * kLog2e, make_div((uint32_t)p.tiles),
+               make_div((uint32_t)heads), make_div((uint32_t)(q_heads / heads)), make_div((uint32_t)p.splits),
+               make_div((uint32_t)(batch->block / 16))};
+    if (p.bytes > 0) a.stat = (float *)((char *)workspace + p.part_bytes);
+    if (dtype == SPCONV_F32) return attention_of<float>(a, stream);
+    if (dtype == SPCONV_F16) return attention_of<_Float16>(a, stream);
+    return attention_of<__bf16>(a, stream);
+}

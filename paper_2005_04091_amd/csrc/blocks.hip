@@ -1,0 +1,363 @@
+// Block scores and block selection (spconv_block_scores, spconv_select_blocks).
+#include "batch.h"
+
+namespace {
+
+constexpr float kInf = __builtin_huge_valf();
+
+// Ones of a ballot, as a signed number.
+__device__ __forceinline__ int bits(uint64_t x) { return (int)__popcll(x); }
+
+struct ScoreArgs {
+    spconv_batch B;
+    const void *q;
+    int64_t q_token, q_head;
+    const float *sums;
+    float *scores;
+    int64_t items;
+    int heads, group, dim, tiles;  // tiles: workgroups of 64 blocks along the table
+    Div tile_div, head_div, group_div;
+    int aligned;
+};
+
+// Eight components of a query from d on (dim is a multiple of 8: all there or none).
+template <typename T>
+__device__ __forceinline__ Floats<8> load_query(const T *p, bool aligned) {
+    Floats<8> r;
+    if (aligned) {
+        constexpr int W = kPer16<T>;
+#pragma unroll
+        for (int i = 0; i < 8; i += W) {
+            const Floats<W> f = load_floats<T, W>(p + i);
+#pragma unroll
+            for (int k = 0; k < W; ++k) r.v[i + k] = f.v[k];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) r.v[i] = (float)p[i];
+    }
+    return r;
+}
+
+// One wave 16 blocks of a (row, head): their key sums stay in registers as the
+// rows of 16x16 fp32 matrix tiles, and the row's (token, head) pairs pass as columns, 16 a
+// tile. Lane l holds components 8*(l/16) .. +8 of every 32 of block l%16, and of pair
+// l%16: the order of the components in a product is free, so each instruction
+// takes one of the eight from every lane.
+template <typename T, int NK>
+__global__ __launch_bounds__(256) void scores_kernel(ScoreArgs a) {
+    const int64_t idx = grid_index();
+    if (idx >= a.items) return;
+    const uint32_t rh = (uint32_t)idx / a.tile_div;
+    const int tile = (int)((uint32_t)idx - rh * a.tile_div.d);
+    const int row = (int)(rh / a.head_div), h = (int)(rh - row * a.head_div.d);
+    const spconv_batch &B = a.B;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int c0 = tile * 64 + wave * 16;
+    if (c0 >= B.max_blocks) return;
+    const Row r = find_row(B, row);
+    const int p1 = r.n > 0 ? r.p0 + r.n - 1 : -1;
+    const int visible = p1 < 0 ? 0 : min(p1 / B.block + 1, B.max_blocks);
+    float *out = a.scores + ((int64_t)row * a.heads + h) * B.max_blocks;
+    if (c0 >= visible) {
+        if (lane < 16 && c0 + lane < B.max_blocks) out[c0 + lane] = -kInf;
+        return;
+    }
+    // Key sums.
+    const int col = lane & 15, part = lane >> 4;
+    Floats<8> s[NK];
+    const int page = c0 + col < visible ? page_of(B, r.b, c0 + col) : -1;
+#pragma unroll
+    for (int k = 0; k < NK; ++k) {
+        const int d = k * 32 + part * 8;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[k].v[i] = 0.0f;
+        if (page >= 0 && d < a.dim) s[k] = load_query(a.sums + ((int64_t)page * a.heads + h) * a.dim + d, true);
+    }
+    // Rows of the result are blocks c0 + 4*part + i, columns pairs.
+    float best[4], inv[4];
+    int key0[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        best[i] = -kInf;
+        const int j = c0 + part * 4 + i;
+        const bool there = __shfl(page, part * 4 + i) >= 0;
+        key0[i] = there ? j * B.block : 0x7fffffff;
+        inv[i] = 1.0f / (float)clamp_int(r.kv - j * B.block, 1, B.block);
+    }
+    const int pairs = r.n * a.group;
+    for (int m0 = 0; m0 < pairs; m0 += 16) {
+        const int m = m0 + col;
+        const int i = (uint32_t)m / a.group_div, g = m - i * (int)a.group_div.d;
+        const int p = m < pairs ? r.p0 + i : -1;
+        const T *q = (const T *)a.q + (int64_t)(r.t0 + i) * a.q_token + (int64_t)(h * a.group + g) * a.q_head;
+        f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int k = 0; k < NK; ++k) {
+            const int d = k * 32 + part * 8;
+            Floats<8> x;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x.v[e] = 0.0f;
+            if (p >= 0 && d < a.dim) x = load_query(q + d, a.aligned);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(s[k].v[e], x.v[e], acc, 0, 0, 0);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (p >= key0[e]) best[e] = fmaxf(best[e], acc[e] * inv[e]);
+    }
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) best[e] = fmaxf(best[e], __shfl_xor(best[e], o));
+    const int j = c0 + part * 4 + (col & 3);
+    const float v = col == 0 ? best[0] : col == 1 ? best[1] : col == 2 ? best[2] : best[3];
+    if (col < 4 && j < B.max_blocks) out[j] = v;
+}
+
+struct SelectArgs {
+    spconv_batch B;
+    const float *scores;
+    int32_t *blocks, *counts;
+    int64_t items;  // rows * heads
+    int heads, keep, sink, local;
+    Div head_div;
+};
+
+// Order of the values as unsigned numbers: 0 stands for "no candidate", -infinity
+// and NaN are 1 (the map of -infinity is 0x007fffff), -0 is +0.
+__device__ __forceinline__ uint32_t order_of(float x) {
+    if (!(x > -kInf)) return 1u;
+    const uint32_t u = __float_as_uint(x + 0.0f);
+    return (u & 0x80000000u) ? ~u : u | 0x80000000u;
+}
+
+// What a row may choose from: n blocks seen, of which [0, sink) and [low, n) are always listed.
+struct Choice {
+    int n, sink, low, want;  // want: how many of the others
+};
+
+__device__ __forceinline__ Choice choice_of(const SelectArgs &a, const Row &r) {
+    const spconv_batch &B = a.B;
+    Choice c;
+    const int p1 = r.n > 0 ? r.p0 + r.n - 1 : -1;
+    c.n = p1 < 0 ? 0 : min(p1 / B.block + 1, B.max_blocks);
+    c.sink = min(a.sink, c.n);
+    c.low = c.n;
+    if (a.local > 0) c.low = clamp_int(max(r.p0, 0) / B.block - a.local + 1, 0, c.n);
+    const int forced = c.low <= c.sink ? c.n : c.sink + c.n - c.low;
+    c.want = a.keep - forced;
+    return c;
+}
+
+// One wave a (row, head) of at most 64*NI blocks, held in registers: the want-th highest
+// value of the candidates is found bit by bit from the top, by counting those that
+// are not below a trial, until exactly `want` are left or the bits are through (ties:
+// the lowest indices of those equal to it). Then the list is written in order.
+template <int NI>
+__global__ __launch_bounds__(256) void select_wave_kernel(SelectArgs a) {
+    const int lane = threadIdx.x & 63;
+    const int64_t item = grid_index() * 4 + (threadIdx.x >> 6);
+    if (item >= a.items) return;
+    const int row = (int)((uint32_t)item / a.head_div);
+    const Row r = find_row(a.B, row);
+    const Choice c = choice_of(a, r);
+    int32_t *blocks = a.blocks + item * a.keep;
+    const int count = min(c.n, a.keep);
+    if (lane == 0) a.counts[item] = count;
+    if (c.n <= a.keep) {
+        for (int i = lane; i < a.keep; i += 64) blocks[i] = i < c.n ? i : -1;
+        return;
+    }
+    const float *s = a.scores + item * a.B.max_blocks;
+    uint32_t v[NI];
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+        const int j = i * 64 + lane;
+        v[i] = j >= c.sink && j < c.low ? order_of(s[j]) : 0u;
+    }
+    uint32_t cut = 0;  // highest t with want or more candidates >= t
+    int above = -1;    // exactly want candidates are >= cut, once known
+    if (c.want > 0) {
+        for (int bit = 31; bit >= 0; --bit) {
+            const uint32_t t = cut | (1u << bit);
+            int n = 0;
+#pragma unroll
+            for (int i = 0; i < NI; ++i) n += bits(__ballot(v[i] >= t));
+            if (n >= c.want) {
+                cut = t;
+                above = n;
+                if (n == c.want) break;
+            }
+        }
+    }
+    // Of those equal to the cut, how many are taken (all, if exactly want are not below it).
+    int ties = 0x7fffffff;
+    if (c.want <= 0) {
+        cut = 0xffffffffu;
+        ties = 0;
+    } else if (above != c.want) {
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < NI; ++i) n += bits(__ballot(v[i] > cut));
+        ties = c.want - n;
+    }
+    int at = 0;
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+        const int j = i * 64 + lane;
+        const uint64_t below = (1ull << lane) - 1;
+        const uint64_t eq = __ballot(v[i] == cut);
+        const bool tie = v[i] == cut && bits(eq & below) < ties;
+        const bool take = j < c.n && (j < c.sink || j >= c.low || v[i] > cut || tie);
+        if (ties != 0x7fffffff) ties = max(0, ties - bits(eq));
+        const uint64_t all = __ballot(take);
+        const int pos = at + bits(all & below);
+        if (take && pos < a.keep) blocks[pos] = j;
+        at += bits(all);
+    }
+    for (int i = at + lane; i < a.keep; i += 64) blocks[i] = -1;
+}
+
+// One workgroup of 1024 threads a (row, head) of more blocks: wave w takes the w-th
+// sixteenth of them, in `per` steps of 64, from the cache each time (a count over all is one pass).
+__global__ __launch_bounds__(1024) void select_block_kernel(SelectArgs a, int per) {
+    __shared__ int counts[2][16];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t item = grid_index();
+    if (item >= a.items) return;
+    const int row = (int)((uint32_t)item / a.head_div);
+    const Row r = find_row(a.B, row);
+    const Choice c = choice_of(a, r);
+    int32_t *blocks = a.blocks + item * a.keep;
+    const int count = min(c.n, a.keep);
+    if (threadIdx.x == 0) a.counts[item] = count;
+    if (c.n <= a.keep) {
+        for (int i = threadIdx.x; i < a.keep; i += 1024) blocks[i] = i < c.n ? i : -1;
+        return;
+    }
+    const float *s = a.scores + item * a.B.max_blocks;
+    const int first = wave * per * 64;
+    int turn = 0;
+    // Sum over the workgroup of a wave's number, and of the waves before this one.
+    auto total = [&](int n, int &before) {
+        if (lane == 0) counts[turn][wave] = n;
+        __syncthreads();
+        int all = 0;
+        before = 0;
+        for (int w = 0; w < 16; ++w) {
+            if (w < wave) before += counts[turn][w];
+            all += counts[turn][w];
+        }
+        turn ^= 1;  // the next one's slots: nobody is still reading those
+        return all;
+    };
+    auto value = [&](int j) { return j >= c.sink && j < c.low ? order_of(s[j]) : 0u; };
+    uint32_t cut = 0;
+    int above = -1, dummy;
+    if (c.want > 0) {
+        for (int bit = 31; bit >= 0; --bit) {
+            const uint32_t t = cut | (1u << bit);
+            int n = 0;
+            for (int i = 0; i < per; ++i) n += bits(__ballot(value(first + i * 64 + lane) >= t));
+            n = total(n, dummy);
+            if (n >= c.want) {
+                cut = t;
+                above = n;
+                if (n == c.want) break;
+            }
+        }
+    }
+    int ties = 0x7fffffff;
+    if (c.want <= 0) {
+        cut = 0xffffffffu;
+        ties = 0;
+    } else if (above != c.want) {
+        int n = 0, eq = 0, before;
+        for (int i = 0; i < per; ++i) {
+            const uint32_t v = value(first + i * 64 + lane);
+            n += bits(__ballot(v > cut));
+            eq += bits(__ballot(v == cut));
+        }
+        n = total(n, dummy);
+        total(eq, before);
+        ties = max(0, c.want - n - before);
+    }
+    // Taken by this wave, then by those before it, then the list.
+    int mine = 0, at = 0;
+    for (int pass = 0; pass < 2; ++pass) {
+        int left = ties, n = 0;
+        for (int i = 0; i < per; ++i) {
+            const int j = first + i * 64 + lane;
+            const uint32_t v = value(j);
+            const uint64_t below = (1ull << lane) - 1;
+            const uint64_t eq = __ballot(v == cut);
+            const bool tie = v == cut && bits(eq & below) < left;
+            const bool take = j < c.n && (j < c.sink || j >= c.low || v > cut || tie);
+            if (left != 0x7fffffff) left = max(0, left - bits(eq));
+            const uint64_t all = __ballot(take);
+            const int pos = at + n + bits(all & below);
+            if (pass == 1 && take && pos < a.keep) blocks[pos] = j;
+            n += bits(all);
+        }
+        if (pass == 0) mine = total(n, at);
+    }
+    for (int i = mine + (int)threadIdx.x; i < a.keep; i += 1024) blocks[i] = -1;
+}
+
+template <typename T>
+int scores_of(ScoreArgs &a, hipStream_t stream) {
+    const dim3 grid = grid_of(a.items);
+    if (a.dim <= 64)
+        scores_kernel<T, 2><<<grid, 256, 0, stream>>>(a);
+    else if (a.dim <= 128)
+        scores_kernel<T, 4><<<grid, 256, 0, stream>>>(a);
+    else
+        scores_kernel<T, 8><<<grid, 256, 0, stream>>>(a);
+    return launched();
+}
+
+}  // namespace
+
+extern "C" int spconv_block_scores(int dtype, const spconv_batch *batch, const void *q, int64_t q_token, int64_t q_head,
+                                   int q_heads, int heads, int dim, const float *sums, float *scores,
+                                   hipStream_t stream) {
+    if (!batch_ok(batch) || !batch_arrays_ok(batch) || !dtype_ok(dtype) || q == nullptr || sums == nullptr ||
+        scores == nullptr || !heads_ok(q_heads, heads, dim) || q_token < 0 || q_head < 0 || !aligned16(sums))
+        return SPCONV_EINVAL;
+    const int tiles = (batch->max_blocks + 63) / 64;
+    const int64_t rows = rows_of(batch);
+    if (rows * heads * tiles >= ((int64_t)1 << 31)) return SPCONV_EINVAL;
+    ScoreArgs a{*batch, q, q_token, q_head, sums, scores, rows * heads * tiles, heads, q_heads / heads, dim, tiles,
+                make_div((uint32_t)tiles), make_div((uint32_t)heads), make_div((uint32_t)(q_heads / heads)),
+                rows_aligned16(q, q_token, q_head, size_of(dtype))};
+    if (dtype == SPCONV_F32) return scores_of<float>(a, stream);
+    if (dtype == SPCONV_F16) return scores_of<_Float16>(a, stream);
+    return scores_of<__bf16>(a, stream);
+}
+
+extern "C" int spconv_select_blocks(const spconv_batch *batch, int heads, const float *scores, int keep, int sink,
+                                    int local, int32_t *blocks, int32_t *counts, hipStream_t stream) {
+    if (!batch_ok(batch) || !batch_arrays_ok(batch) || scores == nullptr || blocks == nullptr || counts == nullptr ||
+        heads < 1 || heads > 65535 || keep < 1 || sink < 0 || local < 0)
+        return SPCONV_EINVAL;
+    const int64_t always = (int64_t)sink + local + (batch->q_block - 1 + batch->block - 1) / batch->block;
+    const int64_t items = rows_of(batch) * heads;
+    if (keep < always || items >= ((int64_t)1 << 31) || items * keep >= ((int64_t)1 << 40)) return SPCONV_EINVAL;
+    SelectArgs a{*batch, scores, blocks, counts, items, heads, keep, sink, local, make_div((uint32_t)heads)};
+    const int n = (batch->max_blocks + 63) / 64;
+    if (n <= 32) {
+        const dim3 grid = grid_of((items + 3) / 4);
+        if (n <= 4)
+            select_wave_kernel<4><<<grid, 256, 0, stream>>>(a);
+        else if (n <= 8)
+            select_wave_kernel<8><<<grid, 256, 0, stream>>>(a);
+        else if (n <= 16)
+            select_wave_kernel<16><<<grid, 256, 0, stream>>>(a);
+        else
+            select_wave_kernel<32><<<grid, 256, 0, stream>>>(a);
+    } else {
+        select_block_kernel<<<grid_of(items), 1024, 0, stream>>>(a, (n + 15) / 16);
+    }
+    return launched();
+}

@@ -1,0 +1,361 @@
+// Rotary positions and the paged cache's append (spconv_rope, spconv_cache_append).
+//
+// Both only move data: a rotated pair takes four products and a sine and cosine
+// that all heads of a token share, so both are bound by HBM (each element read and
+// written once) or, for single tokens, by the launch.
+//
+// Angles: position * frequency in turns is formed in fp64 and taken to the nearest
+// whole turn there (positions up to 2^31 turn the fastest pair 3e8 times: fp32 would
+// lose the fraction), then the rest, at most half a turn, goes through fp32 sine and
+// cosine of a multiple of pi, a relative error of 2^-24 or so whatever the position.
+#include "batch.h"
+
+namespace {
+
+struct CosSin {
+    float c, s;
+};
+
+__device__ __forceinline__ CosSin rope_angle(int position, double freq, float sign, float amplitude) {
+    const double turns = (double)position * (freq * 0.15915494309189533577);  // 1 / (2 pi)
+    const float half_turns = (float)((turns - rint(turns)) * 2.0);
+    float s, c;
+    sincospif(half_turns, &s, &c);
+    return {c * amplitude, s * amplitude * sign};
+}
+
+// W pairs: x of the first components, y of the second ones (half layout), or, in
+// the interleaved layout of W > 1, 2W neighbours (x then y).
+template <int W, bool INTER>
+__device__ __forceinline__ void rotate(Floats<W> &x, Floats<W> &y, const CosSin (&a)[W]) {
+    if constexpr (INTER && W > 1) {
+#pragma unroll
+        for (int i = 0; i < W / 2; ++i) {
+            const float u = x.v[2 * i], v = x.v[2 * i + 1], p = y.v[2 * i], q = y.v[2 * i + 1];
+            const CosSin m = a[i], n = a[W / 2 + i];
+            x.v[2 * i] = u * m.c - v * m.s;
+            x.v[2 * i + 1] = v * m.c + u * m.s;
+            y.v[2 * i] = p * n.c - q * n.s;
+            y.v[2 * i + 1] = q * n.c + p * n.s;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            const float u = x.v[i], v = y.v[i];
+            x.v[i] = u * a[i].c - v * a[i].s;
+            y.v[i] = v * a[i].c + u * a[i].s;
+        }
+    }
+}
+
+// Where the two vectors of pairs [u*W, u*W + W) start.
+template <int W, bool INTER>
+__device__ __forceinline__ void pair_at(int u, int rot, int &d0, int &d1) {
+    d0 = INTER ? 2 * u * W : u * W;
+    d1 = INTER ? d0 + W : d0 + rot / 2;
+}
+
+struct RopeArgs {
+    const void *x;
+    void *out;
+    int64_t x_token, x_head, o_token, o_head;
+    const int32_t *positions;
+    const double *freq;
+    int64_t tokens;
+    int heads, dim, rot, group;  // group: tokens a workgroup takes at a time
+    Div half, units, row;        // rot/2; vectors of a head (pairs and copies); heads * units
+    float sign, amplitude;
+};
+
+// A workgroup takes `group` tokens: their sines and cosines into LDS, once for all
+// heads, then every (token, head, vector pair) by one thread.
+template <typename T, int W, bool INTER>
+__global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
+    extern __shared__ CosSin table[];
+    const int tid = threadIdx.x;
+    const T *x = (const T *)a.x;
+    T *out = (T *)a.out;
+    const int64_t groups = (a.tokens + a.group - 1) / a.group;
+    for (int64_t g = blockIdx.x; g < groups; g += gridDim.x) {
+        const int64_t t0 = g * a.group;
+        const int n = (int)min((int64_t)a.group, a.tokens - t0);
+        __syncthreads();
+        for (int i = tid; i < n * (int)a.half.d; i += 256) {
+            const int t = (uint32_t)i / a.half;
+            table[i] = rope_angle(a.positions[t0 + t], a.freq[i - t * (int)a.half.d], a.sign, a.amplitude);
+        }
+        __syncthreads();
+        const int total = n * (int)a.row.d;
+        for (int i = tid; i < total; i += 256) {
+            const int t = (uint32_t)i / a.row, r = i - t * (int)a.row.d;
+            const int h = (uint32_t)r / a.units, u = r - h * (int)a.units.d;
+            const T *xr = x + (t0 + t) * a.x_token + h * a.x_head;
+            T *yr = out + (t0 + t) * a.o_token + h * a.o_head;
+            if (u * W < a.rot / 2) {
+                int d0, d1;
+                pair_at<W, INTER>(u, a.rot, d0, d1);
+                Floats<W> p = load_floats<T, W>(xr + d0), q = load_floats<T, W>(xr + d1);
+                CosSin m[W];
+#pragma unroll
+                for (int k = 0; k < W; ++k) m[k] = table[t * (int)a.half.d + u * W + k];
+                rotate<W, INTER>(p, q, m);
+                store_floats<T, W>(yr + d0, p);
+                store_floats<T, W>(yr + d1, q);
+            } else {
+                const int d = a.rot / 2 + u * W;  // rot + (u - rot/2/W) * W
+                if constexpr (W == 1) {
+                    yr[d] = xr[d];
+                } else {
+                    typedef typename VecOf<T, W>::type V;
+                    *reinterpret_cast<V *>(yr + d) = *reinterpret_cast<const V *>(xr + d);
+                }
+            }
+        }
+    }
+}
+
+struct AppendArgs {
+    spconv_batch B;
+    const void *k, *v;
+    int64_t k_token, k_head, v_token, v_head;
+    void *k_cache, *v_cache;
+    float *sums;
+    const int32_t *positions;
+    const double *freq;
+    int64_t items;
+    int heads, dim, rot;
+    Div units;  // vectors of a key (pairs and copies)
+    Div vecs;   // vectors of a value
+    float amplitude;
+};
+
+// One workgroup a (touched page, head). The pages that sequence b touches are items
+// q_start[b]/block + 2b and on: a sequence of n tokens touches n/block + 2 pages at
+// most. Threads hold one vector pair of a key each and walk the page's rows
+// in strides, so that the page's sum is a sum of a thread's rows and then of 256/units
+// threads, always in the same order: no atomics.
+template <typename T, int W, bool INTER>
+__global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
+    __shared__ float part[256 * 2 * W];
+    const int64_t item = grid_index() / a.heads;
+    const int h = (int)(grid_index() - item * a.heads);
+    if (item >= a.items) return;
+    const spconv_batch &B = a.B;
+    const Seq s = find_seq(B, (int)item, B.block, 2);
+    if (s.b < 0 || s.at < 0 || s.n == 0 || s.kv == 0) return;
+    const int from = s.kv - s.n;  // position of the first new token (tokens at negative ones are dropped)
+    const int64_t block64 = max(from, 0) / B.block + (int64_t)s.at;
+    if (block64 > (s.kv - 1) / B.block) return;
+    const int j = (int)block64;
+    const int page = page_of(B, s.b, j);
+    if (page < 0) return;
+    const int s0 = max(from - j * B.block, 0), s1 = min(s.kv - j * B.block, B.block);
+    const int t_off = s.first + j * B.block - from;  // token of slot s: s + t_off
+    const int tid = threadIdx.x;
+    const int64_t base = ((int64_t)page * a.heads + h) * B.block * a.dim;
+    T *kc = (T *)a.k_cache + base, *vc = (T *)a.v_cache + base;
+
+    // Values: copied.
+    const int nv = (s1 - s0) * (int)a.vecs.d;
+    for (int i = tid; i < nv; i += 256) {
+        const int r = (uint32_t)i / a.vecs, c = (i - r * (int)a.vecs.d) * W;
+        const T *src = (const T *)a.v + (int64_t)(s0 + r + t_off) * a.v_token + h * a.v_head + c;
+        T *dst = vc + (int64_t)(s0 + r) * a.dim + c;
+        if constexpr (W == 1) {
+            *dst = *src;
+        } else {
+            typedef typename VecOf<T, W>::type V;
+            *reinterpret_cast<V *>(dst) = *reinterpret_cast<const V *>(src);
+        }
+    }
+
+    // Keys: rotated, stored, summed.
+    const int units = a.units.d, groups = 256 / units;
+    const int g = (uint32_t)tid / a.units, u = tid - g * units;
+    const bool pair = u * W < a.rot / 2;
+    int d0, d1 = 0;
+    if (pair)
+        pair_at<W, INTER>(u, a.rot, d0, d1);
+    else
+        d0 = a.rot / 2 + u * W;
+    Floats<W> sum0, sum1;
+#pragma unroll
+    for (int i = 0; i < W; ++i) sum0.v[i] = sum1.v[i] = 0.0f;
+    if (g < groups) {
+        const int r0 = a.sums ? 0 : s0;
+        for (int r = r0 + g; r < s1; r += groups) {
+            T *dst = kc + (int64_t)r * a.dim;
+            Floats<W> p, q;
+#pragma unroll
+            for (int i = 0; i < W; ++i) q.v[i] = 0.0f;
+            if (r < s0) {
+                p = load_floats<T, W>(dst + d0);
+                if (pair) q = load_floats<T, W>(dst + d1);
+            } else {
+                const int t = r + t_off;
+                const T *src = (const T *)a.k + (int64_t)t * a.k_token + h * a.k_head;
+                p = load_floats<T, W>(src + d0);
+                if (pair) {
+                    q = load_floats<T, W>(src + d1);
+                    const int position = a.positions ? a.positions[t] : j * B.block + r;
+                    CosSin m[W];
+#pragma unroll
+                    for (int k = 0; k < W; ++k) m[k] = rope_angle(position, a.freq[u * W + k], 1.0f, a.amplitude);
+                    rotate<W, INTER>(p, q, m);
+                    q = store_floats<T, W>(dst + d1, q);
+                }
+                p = store_floats<T, W>(dst + d0, p);
+            }
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+                sum0.v[i] += p.v[i];
+                sum1.v[i] += q.v[i];
+            }
+        }
+    }
+    if (a.sums == nullptr) return;
+    if (g < groups) {
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            part[g * a.dim + d0 + i] = sum0.v[i];
+            if (pair) part[g * a.dim + d1 + i] = sum1.v[i];
+        }
+    }
+    __syncthreads();
+    float *sums = a.sums + ((int64_t)page * a.heads + h) * a.dim;
+    for (int d = tid; d < a.dim; d += 256) {
+        float t = 0.0f;
+        for (int k = 0; k < groups; ++k) t += part[k * a.dim + d];
+        sums[d] = t;
+    }
+}
+
+// Whether heads of dim components split into vectors of w: whole vectors of pairs, whole ones behind them.
+bool splits_into(int dim, int rot, int w) { return (rot / 2) % w == 0 && (dim - rot) % w == 0; }
+
+template <typename T, int W>
+int launch_rope(const RopeArgs &a, bool inter, int blocks, size_t lds, hipStream_t stream) {
+    if (inter)
+        rope_kernel<T, W, true><<<blocks, 256, lds, stream>>>(a);
+    else
+        rope_kernel<T, W, false><<<blocks, 256, lds, stream>>>(a);
+    return launched();
+}
+
+template <typename T>
+int rope_of(RopeArgs &a, bool inter, hipStream_t stream) {
+    constexpr int V = kPer16<T>;
+    const bool vec = splits_into(a.dim, a.rot, V) && rows_aligned16(a.x, a.x_token, a.x_head, sizeof(T)) &&
+                     rows_aligned16(a.out, a.o_token, a.o_head, sizeof(T));
+    const int units = (a.dim - a.rot / 2) / (vec ? V : 1);
+    a.units = make_div((uint32_t)units);
+    a.row = make_div((uint32_t)units * (uint32_t)a.heads);
+    // Tokens a workgroup takes at a time: about 1024 vector pairs, sines within 32 KiB, and
+    // workgroups for every CU as long as there are tokens for it.
+    int64_t group = std::max<int64_t>(1, 1024 / ((int64_t)units * a.heads));
+    group = std::min<int64_t>(group, std::max<int64_t>(1, a.tokens / 1024));
+    group = std::min<int64_t>(group, 4096 / std::max(a.rot / 2, 1));
+    a.group = (int)group;
+    const int64_t groups = (a.tokens + group - 1) / group;
+    const int blocks = (int)std::min<int64_t>(groups, 1 << 20);
+    const size_t lds = (size_t)group * (a.rot / 2) * sizeof(CosSin);
+    return vec ? launch_rope<T, V>(a, inter, blocks, lds, stream) : launch_rope<T, 1>(a, inter, blocks, lds, stream);
+}
+
+template <typename T, int W>
+int launch_append(AppendArgs &a, bool inter, hipStream_t stream) {
+    a.units = make_div((uint32_t)((a.dim - a.rot / 2) / W));
+    a.vecs = make_div((uint32_t)(a.dim / W));
+    const dim3 grid = grid_of(a.items * a.heads);
+    if (inter)
+        append_kernel<T, W, true><<<grid, 256, 0, stream>>>(a);
+    else
+        append_kernel<T, W, false><<<grid, 256, 0, stream>>>(a);
+    return launched();
+}
+
+template <typename T>
+int append_of(AppendArgs &a, bool inter, hipStream_t stream) {
+    constexpr int V = kPer16<T>;
+    const bool vec = splits_into(a.dim, a.rot, V) && rows_aligned16(a.k, a.k_token, a.k_head, sizeof(T)) &&
+                     rows_aligned16(a.v, a.v_token, a.v_head, sizeof(T));
+    return vec ? launch_append<T, V>(a, inter, stream) : launch_append<T, 1>(a, inter, stream);
+}
+
+}  // namespace
+
+extern "C" int spconv_batch_rows(const spconv_batch *batch, int64_t *rows) {
+    if (!batch_ok(batch) || rows == nullptr) return SPCONV_EINVAL;
+    *rows = rows_of(batch);
+    return SPCONV_OK;
+}
+
+extern "C" int spconv_rope_frequencies(int rot, double base, const spconv_rope_scaling *scaling, double *freq) {
+    if (freq == nullptr || rot < 2 || rot % 2 != 0 || !std::isfinite(base) || base <= 0.0) return SPCONV_EINVAL;
+    const int kind = scaling ? scaling->kind : SPCONV_ROPE_PLAIN;
+    if (kind < SPCONV_ROPE_PLAIN || kind > SPCONV_ROPE_BY_PARTS) return SPCONV_EINVAL;
+    if (kind != SPCONV_ROPE_PLAIN && !(std::isfinite(scaling->factor) && scaling->factor >= 1.0)) return SPCONV_EINVAL;
+    if (kind == SPCONV_ROPE_BASE) {
+        if (rot == 2) return SPCONV_EINVAL;
+        base *= std::pow(scaling->factor, (double)rot / (rot - 2));
+        if (!std::isfinite(base)) return SPCONV_EINVAL;
+    }
+    if (kind == SPCONV_ROPE_BY_PARTS &&
+        !(scaling->low > 0.0 && scaling->high > scaling->low && std::isfinite(scaling->high) &&
+          scaling->original > 0.0 && std::isfinite(scaling->original)))
+        return SPCONV_EINVAL;
+    for (int i = 0; i < rot / 2; ++i) {
+        double f = std::pow(base, -2.0 * i / rot);
+        if (kind == SPCONV_ROPE_LINEAR) f /= scaling->factor;
+        if (kind == SPCONV_ROPE_BY_PARTS) {
+            const double turns = scaling->original * f / 6.283185307179586477;  // original / wavelength
+            double t = (turns - scaling->low) / (scaling->high - scaling->low);
+            t = t < 0.0 ? 0.0 : t > 1.0 ? 1.0 : t;
+            f = (1.0 - t) * f / scaling->factor + t * f;
+        }
+        freq[i] = f;
+    }
+    return SPCONV_OK;
+}
+
+extern "C" int spconv_rope(int dtype, const void *x, int64_t x_token, int64_t x_head, int64_t tokens, int heads, int dim,
+                           const int32_t *positions, const double *freq, int rot, uint32_t flags, float amplitude,
+                           void *out, int64_t out_token, int64_t out_head, hipStream_t stream) {
+    if (!dtype_ok(dtype) || x == nullptr || out == nullptr || positions == nullptr || (freq == nullptr && rot != 0))
+        return SPCONV_EINVAL;
+    if (tokens < 1 || tokens > 0x7fffffff || heads < 1 || heads > 65535 || dim < 1 || dim > 1024 || rot < 0 ||
+        rot > dim || rot % 2 != 0 || (flags & ~(SPCONV_ROPE_INTERLEAVED | SPCONV_ROPE_INVERSE)) != 0 ||
+        !std::isfinite(amplitude) || x_token < 0 || x_head < 0 || !out_strides_ok(tokens, heads, dim, out_token, out_head))
+        return SPCONV_EINVAL;
+    if (x == out && (x_token != out_token || x_head != out_head)) return SPCONV_EINVAL;
+    RopeArgs a{x, out, x_token, x_head, out_token, out_head, positions, freq, tokens, heads, dim, rot, 1,
+               make_div((uint32_t)std::max(rot / 2, 1)), {}, {}, (flags & SPCONV_ROPE_INVERSE) ? -1.0f : 1.0f, amplitude};
+    if (rot == 0) a.half.d = 0;  // no angles
+    const bool inter = (flags & SPCONV_ROPE_INTERLEAVED) != 0;
+    if (dtype == SPCONV_F32) return rope_of<float>(a, inter, stream);
+    if (dtype == SPCONV_F16) return rope_of<_Float16>(a, inter, stream);
+    return rope_of<__bf16>(a, inter, stream);
+}
+
+extern "C" int spconv_cache_append(int dtype, const spconv_batch *batch, const void *k, int64_t k_token, int64_t k_head,
+                                   const void *v, int64_t v_token, int64_t v_head, int heads, int dim,
+                                   const int32_t *positions, const double *freq, int rot, uint32_t flags,
+                                   float amplitude, void *k_cache, void *v_cache, float *sums, hipStream_t stream) {
+    if (!batch_ok(batch) || !batch_arrays_ok(batch) || !dtype_ok(dtype) || k == nullptr || v == nullptr ||
+        k_cache == nullptr || v_cache == nullptr)
+        return SPCONV_EINVAL;
+    if (!heads_ok(heads, heads, dim) || rot < 0 || rot > dim || rot % 2 != 0 || (freq == nullptr) != (rot == 0) ||
+        (flags & ~SPCONV_ROPE_INTERLEAVED) != 0 || !std::isfinite(amplitude) || k_token < 0 || k_head < 0 ||
+        v_token < 0 || v_head < 0 || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(sums))
+        return SPCONV_EINVAL;
+    // Touched pages of all sequences; one each without q_start.
+    const int64_t items =
+        batch->q_start ? batch->tokens / batch->block + 2 * (int64_t)batch->sequences : (int64_t)batch->sequences;
+    if (items > 0x7fffffff) return SPCONV_EINVAL;
+    AppendArgs a{*batch, k, v, k_token, k_head, v_token, v_head, k_cache, v_cache, sums, positions, freq, items, heads,
+                 dim, rot, {}, {}, amplitude};
+    const bool inter = (flags & SPCONV_ROPE_INTERLEAVED) != 0;
+    if (dtype == SPCONV_F32) return append_of<float>(a, inter, stream);
+    if (dtype == SPCONV_F16) return append_of<_Float16>(a, inter, stream);
+    return append_of<__bf16>(a, inter, stream);
+}
