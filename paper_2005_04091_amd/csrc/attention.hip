@@ -76,31 +76,33 @@ struct AttnArgs {
     void *out;
     int64_t o_token, o_head;
     float *lse;
-    float *part, *stat;  // workspace: [item][split][16][dim], [item][split][16][2]
+    float *part, *stat;  // workspace: [item][split][tile_pairs][dim], [item][split][tile_pairs][2]
     int64_t items;       // rows * heads * tiles
-    int heads, group, dim, keep, tiles, splits, q_aligned;
-    float scale2;  // scale / ln 2
-    Div tile_div, head_div, group_div, split_div, slab_div;
+    int heads, group, dim, keep, tiles, splits, q_aligned, o_aligned;
+    int tile_pairs;      // pairs of a tile
+    float scale2;        // scale / ln 2
+    Div tile_div, head_div, group_div, split_div, slab_div, pair_div;
 };
 
-// The 16 (token, head) pairs of a tile of a row, token by token: pair m is token m / group, head m % group.
+// The (token, head) pairs of a tile of a row, token by token: pair m is token m / group, head m % group.
 struct Pairs {
     Row r;
-    int h, m0, last;  // last: position of the tile's last token, -1 if it has none
+    int h, m0, end;   // pairs [m0, end)
+    int last;         // position of the tile's last token, -1 if it has none
     int64_t rh;
 };
 
 __device__ __forceinline__ Pairs find_pairs(const AttnArgs &a, uint32_t item) {
     Pairs p;
     const uint32_t rh = item / a.tile_div;
-    p.m0 = (int)(item - rh * a.tile_div.d) * 16;
+    p.m0 = (int)(item - rh * a.tile_div.d) * a.tile_pairs;
     const int row = (int)(rh / a.head_div);
     p.h = (int)(rh - row * a.head_div.d);
     p.rh = rh;
     p.r = find_row(a.B, row);
-    const int end = min(p.r.n * a.group, p.m0 + 16);
-    p.last = end > p.m0 ? p.r.p0 + (int)((uint32_t)(end - 1) / a.group_div) : -1;
-    if (end <= p.m0) p.r.n = 0;
+    p.end = min(p.r.n * a.group, p.m0 + a.tile_pairs);
+    p.last = p.end > p.m0 ? p.r.p0 + (int)((uint32_t)(p.end - 1) / a.group_div) : -1;
+    if (p.end <= p.m0) p.r.n = 0;
     return p;
 }
 
@@ -348,7 +350,7 @@ __global__ __launch_bounds__(256) void rows_kernel(AttnArgs a) {
         w_sum[wave][col] = sum;
     }
     __syncthreads();
-    const int pairs = min(16, P.r.n * a.group - P.m0);
+    const int pairs = P.end - P.m0;
     for (int i = tid; i < pairs * DP; i += 256) {
         const int c = i / DP, d = i % DP;
         if (d >= D) continue;
@@ -378,30 +380,430 @@ __global__ __launch_bounds__(256) void rows_kernel(AttnArgs a) {
     }
 }
 
+// ---- many pairs: 32x32 tiles, keys and values staged in LDS for all waves ----
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+__device__ __forceinline__ f32x16 mma32(frag_t<__bf16> a, frag_t<__bf16> b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 mma32(frag_t<_Float16> a, frag_t<_Float16> b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 mma32(frag_t<float> a, frag_t<float> b, f32x16 c) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[i], b[i], c, 0, 0, 0);
+    return c;
+}
+
+// Max and sum over the two lanes that hold one column (lanes l, l+32).
+__device__ __forceinline__ float half_max(float x) {
+    const uint32_t u = __float_as_uint(x);
+    const auto a = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+}
+__device__ __forceinline__ float half_sum(float x) {
+    const uint32_t u = __float_as_uint(x);
+    const auto a = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return __uint_as_float(a[0]) + __uint_as_float(a[1]);
+}
+
+// Where unit c (16 bytes) of row r lies in a staged tile of UPR units a row: keys are
+// read by 16 lanes at the same unit of 16 rows, values (16-bit ones) by 32 lanes at four units of
+// four rows; each such group of reads touches all 64 banks once.
+template <int UPR>
+__device__ __forceinline__ int key_unit(int r, int c) {
+    return UPR >= 16 ? c ^ (r & 15) : c ^ ((r >> 1) & (UPR - 1));
+}
+template <int UPR, int SIZE>
+__device__ __forceinline__ int value_unit(int r, int c) {
+    if (SIZE == 4) return c;
+    return UPR >= 16 ? c ^ ((r & 3) << 2) : c ^ (((r >> 1) & 1) << 2);
+}
+
+// One workgroup a (row, head, 32 pairs for each of its waves, share of the row's keys): the waves
+// walk the keys together, KT at a time, staged in LDS, each with the queries, the
+// statistics and the output of its own 32 pairs in registers.
+// While a tile is computed the next one is on its way to registers; it is put into the other
+// half of the LDS behind the computation, one barrier a tile.
+// The running maximum is raised only when a tile passes it by a factor of 2^8 or more: weights up
+// to 2^8 are as exact as those up to 1, and the output is rescaled a few times a row instead of
+// nearly every tile.
+template <typename T, int NK, int KT, int THREADS>
+__global__ __launch_bounds__(THREADS) void tiles_kernel(AttnArgs a) {
+    constexpr int DP = NK * 32, W = kPer16<T>, UPR = DP / W, SIZE = (int)sizeof(T);
+    constexpr int NL = KT * UPR / THREADS;  // units a thread stages of a tile's keys, and of its values
+    constexpr int NS = KT / 16, NB = KT / 32, NQ = DP / 16, NT = DP / 32;
+    __shared__ __attribute__((aligned(16))) T lds[2][2][KT * DP];
+    __shared__ int e_block[kEntries], e_page[kEntries];
+    typedef typename VecOf<T, W>::type V;
+    typedef typename VecOf<T, 4>::type V4;
+
+    int64_t idx = grid_index();
+    const int64_t all = a.items * a.splits;
+    if (idx >= all) return;
+    if (gridDim.y == 1) idx = xcd_linear_id((int)idx, (int)all);
+    const uint32_t item = (uint32_t)idx / a.split_div;
+    const int split = (int)((uint32_t)idx - item * a.split_div.d);
+    const Pairs P = find_pairs(a, item);
+    if (P.r.n == 0) return;
+    const spconv_batch &B = a.B;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 31, half = lane >> 5;
+    const int D = a.dim, spb = B.block >> 4;
+
+    // Query of this lane's column. The sign of the scale goes into it.
+    const int m = P.m0 + wave * 32 + col, tok = (uint32_t)m / a.group_div;
+    const bool live = m < P.end;
+    const int pos = live ? P.r.p0 + tok : -1;
+    const float scale2 = fabsf(a.scale2);
+    const int64_t head = (int64_t)P.h * a.group + (m - tok * a.group);
+    frag_t<T> q[NQ];
+    {
+        const T *src = (const T *)a.q + (int64_t)(P.r.t0 + tok) * a.q_token + head * a.q_head;
+#pragma unroll
+        for (int k = 0; k < NQ; ++k) {
+            const int d = k * 16 + half * 8;
+            q[k] = zero_frag<T>();
+            if (live && d < D) {
+                if (a.q_aligned) {
+                    q[k] = *reinterpret_cast<const frag_t<T> *>(src + d);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) q[k][i] = src[d + i];
+                }
+                if (a.scale2 < 0.0f) q[k] = -q[k];
+            }
+        }
+    }
+    const int first_pos = P.r.p0 + (int)((uint32_t)P.m0 / a.group_div);
+    // Of this wave's pairs: the first and last positions.
+    const int w0 = P.m0 + wave * 32;
+    const int wave_first = P.r.p0 + (int)((uint32_t)w0 / a.group_div);
+    const int wave_last = w0 < P.end ? P.r.p0 + (int)((uint32_t)(min(w0 + 32, P.end) - 1) / a.group_div) : -1;
+
+    int entries = 0;
+    if (P.last >= 0) entries = min(P.last / B.block + 1, B.max_blocks);
+    if (a.blocks) entries = P.last < 0 ? 0 : a.counts ? clamp_int(a.counts[P.rh], 0, a.keep) : a.keep;
+    const int64_t slabs = (int64_t)entries * spb;
+    const int64_t per = ((slabs + NS - 1) / NS + a.splits - 1) / a.splits * NS;
+    const int64_t s_lo = min(per * split, slabs), s_hi = min(s_lo + per, slabs);
+
+    f32x16 o[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[t][i] = 0.0f;
+    float top = -kInf, sum = 0.0f;  // top: of the products before scaling
+
+    for (int e0 = s_lo < s_hi ? (int)(s_lo / spb) : 0; (int64_t)e0 * spb < s_hi; e0 += kEntries) {
+        __syncthreads();
+        for (int i = tid; i < kEntries; i += THREADS) {
+            const int e = e0 + i;
+            int j = -1, page = -1;
+            if (e < entries) {
+                j = a.blocks ? a.blocks[P.rh * a.keep + e] : e;
+                if (j >= 0 && j <= P.last / B.block && j < B.max_blocks) page = page_of(B, P.r.b, j);
+            }
+            e_block[i] = j;
+            e_page[i] = page;
+        }
+        __syncthreads();
+        const int lo = (int)(max(s_lo, (int64_t)e0 * spb) - (int64_t)e0 * spb);
+        const int hi = (int)(min(s_hi, ((int64_t)e0 + kEntries) * spb) - (int64_t)e0 * spb);
+
+        // First key of slab s and its place in the cache; -1 where nothing of it is seen.
+        auto slab = [&](int s, int64_t &base) {
+            base = 0;
+            if (s >= hi) return -1;
+            const int e = (uint32_t)s / a.slab_div, sub = s - e * spb;
+            const int page = __builtin_amdgcn_readfirstlane(e_page[e]);
+            const int key0 = __builtin_amdgcn_readfirstlane(e_block[e]) * B.block + sub * 16;
+            base = (((int64_t)page * a.heads + P.h) * B.block + sub * 16) * D;
+            return page >= 0 && key0 <= P.last ? key0 : -1;
+        };
+        V kr[NL], vr[NL];
+        auto fetch = [&](int s0) {
+#pragma unroll
+            for (int i = 0; i < NL; ++i) {
+                const int row = (i * THREADS + wave * 64) / UPR + lane / UPR, c = lane % UPR;
+                int64_t base;
+                const int key0 = slab(s0 + (i * THREADS + wave * 64) / UPR / 16, base);
+#pragma unroll
+                for (int e = 0; e < W; ++e) kr[i][e] = vr[i][e] = (T)0.0f;
+                if (key0 >= 0 && c * W < D) {
+                    const int64_t at = base + (row & 15) * D + c * W;
+                    kr[i] = *reinterpret_cast<const V *>((const T *)a.k_cache + at);
+                    // Values that no pair sees stay zero, whatever lies there: their weights
+                    // are zero, and zero times infinity is not.
+                    if (key0 + (row & 15) <= P.last) vr[i] = *reinterpret_cast<const V *>((const T *)a.v_cache + at);
+                }
+            }
+        };
+        // Whether every pair of the workgroup sees the whole tile.
+        auto whole = [&](int s0) {
+            bool w = true;
+            int64_t base;
+#pragma unroll
+            for (int n = 0; n < NS; ++n) {
+                const int key0 = slab(s0 + n, base);
+                w = w && key0 >= 0 && key0 + 15 <= first_pos;
+            }
+            return w;
+        };
+        // The fetched tile into LDS. In a tile that some see a part of, values that are not finite are
+        // taken out (returns whether there are any); they come back in a pass of their own.
+        auto put = [&](int buf, bool full) {
+            bool odd = false;
+#pragma unroll
+            for (int i = 0; i < NL; ++i) {
+                const int row = (i * THREADS + wave * 64) / UPR + lane / UPR, c = lane % UPR;
+                if (!full) {
+#pragma unroll
+                    for (int e = 0; e < W; ++e)
+                        if (not_finite((float)vr[i][e])) {
+                            odd = true;
+                            vr[i][e] = (T)0.0f;
+                        }
+                }
+                *reinterpret_cast<V *>(&lds[buf][0][row * DP + key_unit<UPR>(row, c) * W]) = kr[i];
+                *reinterpret_cast<V *>(&lds[buf][1][row * DP + value_unit<UPR, SIZE>(row, c) * W]) = vr[i];
+            }
+            return odd;
+        };
+        // Eight keys of values, as rows of the second product: components t*32 + col, slots of step n.
+        auto value_frag = [&](const T *v, int t, int n) {
+            frag_t<T> f;
+            if constexpr (SIZE == 2) {
+                typedef short s16x4 __attribute__((ext_vector_type(4)));
+                typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+                union {
+                    s16x4 h[2];
+                    frag_t<T> f;
+                } u;
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    const int r = n * 16 + b * 8 + half * 4 + ((lane & 15) >> 2);
+                    const int d = t * 32 + ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
+                    const T *src = v + r * DP + value_unit<UPR, SIZE>(r, d / W) * W + (d & (W - 1));
+                    u.h[b] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)src);
+                }
+                f = u.f;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) f[i] = v[(n * 16 + (i >> 2) * 8 + half * 4 + (i & 3)) * DP + t * 32 + col];
+            }
+            return f;
+        };
+
+        fetch(lo);
+        bool full = whole(lo);
+        bool odd = put(0, full);
+        if (full)
+            __syncthreads();
+        else
+            odd = __syncthreads_or(odd);
+        int buf = 0;
+        for (int s0 = lo; s0 < hi; s0 += NS, buf ^= 1) {
+            const bool more = s0 + NS < hi;
+            if (more) fetch(s0 + NS);
+            int key0[NS], low = 0x7fffffff;
+            int64_t base;
+#pragma unroll
+            for (int n = 0; n < NS; ++n) {
+                key0[n] = slab(s0 + n, base);
+                if (key0[n] >= 0) low = min(low, key0[n]);
+            }
+            const T *ks = lds[buf][0], *vs = lds[buf][1];
+            if (low <= wave_last) {
+                f32x16 x[NB];
+#pragma unroll
+                for (int b = 0; b < NB; ++b) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) x[b][i] = 0.0f;
+#pragma unroll
+                    for (int k = 0; k < NQ; ++k) {
+                        const int r = b * 32 + col;
+                        frag_t<T> f;
+                        if constexpr (SIZE == 2) {
+                            f = *reinterpret_cast<const frag_t<T> *>(ks + r * DP + key_unit<UPR>(r, k * 2 + half) * W);
+                        } else {
+                            union {
+                                V h[2];
+                                frag_t<T> f;
+                            } u;
+                            u.h[0] = *reinterpret_cast<const V *>(ks + r * DP + key_unit<UPR>(r, k * 4 + half * 2) * W);
+                            u.h[1] = *reinterpret_cast<const V *>(ks + r * DP + key_unit<UPR>(r, k * 4 + half * 2 + 1) * W);
+                            f = u.f;
+                        }
+                        x[b] = mma32(f, q[k], x[b]);
+                    }
+                }
+                bool cut = !full;
+                if (cut) {  // this wave may see all of it
+                    cut = false;
+#pragma unroll
+                    for (int n = 0; n < NS; ++n) cut = cut || key0[n] < 0 || key0[n] + 15 > wave_first;
+                }
+                if (cut) {
+#pragma unroll
+                    for (int b = 0; b < NB; ++b)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const int k0 = key0[b * 2 + (i >> 3)], key = k0 + ((i >> 2) & 1) * 8 + half * 4 + (i & 3);
+                            x[b][i] = k0 >= 0 && key <= pos ? x[b][i] : -kInf;
+                        }
+                }
+                float hi32 = -kInf;
+#pragma unroll
+                for (int b = 0; b < NB; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) hi32 = fmaxf(hi32, x[b][i]);
+                hi32 = half_max(hi32);
+                if (__ballot((hi32 - top) * scale2 > 8.0f)) {
+                    const float next = fmaxf(top, hi32);
+                    const float shrink = next == -kInf ? 1.0f : __builtin_amdgcn_exp2f((top - next) * scale2);
+                    top = next;
+                    sum *= shrink;
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) o[t] *= shrink;
+                }
+                const float ref = top == -kInf ? 0.0f : -top * scale2;
+                float total[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int b = 0; b < NB; ++b) {
+                    frag_t<T> w[2];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const float p = __builtin_amdgcn_exp2f(fmaf(x[b][i], scale2, ref));
+                        total[i & 3] += p;
+                        w[i >> 3][i & 7] = (T)p;
+                    }
+#pragma unroll
+                    for (int n = 0; n < 2; ++n)
+#pragma unroll
+                        for (int t = 0; t < NT; ++t) o[t] = mma32(value_frag(vs, t, b * 2 + n), w[n], o[t]);
+                }
+                sum += (total[0] + total[1]) + (total[2] + total[3]);
+            }
+            if (odd) {
+                // Values that are not finite, where some see a part of the tile only: products of
+                // who sees a key (1 or 0) with where its value is +infinity or NaN, then
+                // -infinity or NaN, say which outputs take part.
+                for (int sign = 0; sign < 2; ++sign) {
+                    __syncthreads();
+#pragma unroll
+                    for (int i = 0; i < NL; ++i) {
+                        const int row = (i * THREADS + wave * 64) / UPR + lane / UPR, c = lane % UPR;
+                        const int k0 = slab(s0 + (i * THREADS + wave * 64) / UPR / 16, base);
+                        V v;
+#pragma unroll
+                        for (int e = 0; e < W; ++e) v[e] = (T)0.0f;
+                        if (k0 >= 0 && k0 + (row & 15) <= P.last && c * W < D) {
+                            const V x = *reinterpret_cast<const V *>((const T *)a.v_cache + base + (row & 15) * D + c * W);
+#pragma unroll
+                            for (int e = 0; e < W; ++e) {
+                                const float f = (float)x[e];
+                                v[e] = (T)(f != f || f == (sign ? -kInf : kInf) ? 1.0f : 0.0f);
+                            }
+                        }
+                        *reinterpret_cast<V *>(&lds[buf][1][row * DP + value_unit<UPR, SIZE>(row, c) * W]) = v;
+                    }
+                    __syncthreads();
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        f32x16 hit;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) hit[i] = 0.0f;
+#pragma unroll
+                        for (int n = 0; n < NS; ++n) {
+                            frag_t<T> w;
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) {
+                                const int key = key0[n] + (i >> 2) * 8 + half * 4 + (i & 3);
+                                w[i] = (T)(key0[n] >= 0 && key <= pos ? 1.0f : 0.0f);
+                            }
+                            hit = mma32(value_frag(vs, t, n), w, hit);
+                        }
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            if (hit[i] > 0.0f) o[t][i] += sign ? -kInf : kInf;
+                    }
+                }
+            }
+            if (more) {
+                full = whole(s0 + NS);
+                odd = put(buf ^ 1, full);
+                if (full)
+                    __syncthreads();
+                else
+                    odd = __syncthreads_or(odd);
+            }
+        }
+    }
+    if (!live) return;
+    sum = half_sum(sum);
+    const float ref = top == -kInf ? 0.0f : top * scale2;
+    if (a.splits == 1) {
+        T *dst = (T *)a.out + (int64_t)(P.r.t0 + tok) * a.o_token + head * a.o_head;
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                const int d = t * 32 + (i >> 2) * 8 + half * 4;
+                if (d >= D) continue;
+                V4 v;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = (T)weighted(o[t][i + e], sum);
+                if (a.o_aligned) {
+                    *reinterpret_cast<V4 *>(dst + d) = v;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) dst[d + e] = v[e];
+                }
+            }
+        if (a.lse && half == 0) a.lse[(int64_t)(P.r.t0 + tok) * (a.heads * a.group) + head] = log_sum(ref, sum);
+    } else {
+        const int64_t at = ((int64_t)item * a.splits + split) * a.tile_pairs + wave * 32 + col;
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                const int d = t * 32 + (i >> 2) * 8 + half * 4;
+                if (d < D)
+                    *reinterpret_cast<f32x4 *>(a.part + at * D + d) = f32x4{o[t][i], o[t][i + 1], o[t][i + 2], o[t][i + 3]};
+            }
+        if (half == 0) {
+            a.stat[at * 2] = top == -kInf ? -kInf : top * scale2;
+            a.stat[at * 2 + 1] = sum;
+        }
+    }
+}
+
 // Joins the shares of a pair: one workgroup a (row, head, tile, pair).
 template <typename T>
 __global__ __launch_bounds__(256) void join_kernel(AttnArgs a) {
     const int64_t idx = grid_index();
-    if (idx >= a.items * 16) return;
-    const uint32_t item = (uint32_t)(idx >> 4);
-    const int c = (int)(idx & 15);
+    if (idx >= a.items * a.tile_pairs) return;
+    const uint32_t item = (uint32_t)idx / a.pair_div;
+    const int c = (int)((uint32_t)idx - item * a.pair_div.d);
     const Pairs P = find_pairs(a, item);
-    if (P.r.n == 0 || P.m0 + c >= P.r.n * a.group) return;
-    const float *stat = a.stat + ((int64_t)item * a.splits * 16 + c) * 2;
-    const float *part = a.part + ((int64_t)item * a.splits * 16 + c) * a.dim;
+    if (P.r.n == 0 || P.m0 + c >= P.end) return;
+    const int step = a.tile_pairs;  // from share to share
+    const float *stat = a.stat + ((int64_t)item * a.splits * step + c) * 2;
+    const float *part = a.part + ((int64_t)item * a.splits * step + c) * a.dim;
     float mx = -kInf;
-    for (int s = 0; s < a.splits; ++s) mx = fmaxf(mx, stat[s * 32]);
+    for (int s = 0; s < a.splits; ++s) mx = fmaxf(mx, stat[s * step * 2]);
     const int m = P.m0 + c, tok = (uint32_t)m / a.group_div, g = P.h * a.group + (m - tok * a.group);
     const int d = threadIdx.x;
     if (d >= a.dim) return;
     const float ref = mx == -kInf ? 0.0f : mx;
     float acc = 0.0f, l = 0.0f;
     for (int s = 0; s < a.splits; ++s) {
-        const float x = stat[s * 32], y = stat[s * 32 + 1];
+        const float x = stat[s * step * 2], y = stat[s * step * 2 + 1];
         if (x == -kInf && y == 0.0f) continue;
         const float f = __builtin_amdgcn_exp2f(x - ref);
         l += f * y;
-        acc += f * part[(int64_t)s * 16 * a.dim + d];
+        acc += f * part[(int64_t)s * step * a.dim + d];
     }
     ((T *)a.out)[(int64_t)(P.r.t0 + tok) * a.o_token + (int64_t)g * a.o_head + d] = (T)weighted(acc, l);
     if (a.lse && d == 0) a.lse[(int64_t)(P.r.t0 + tok) * (a.heads * a.group) + g] = log_sum(ref, l);
@@ -409,41 +811,70 @@ __global__ __launch_bounds__(256) void join_kernel(AttnArgs a) {
 
 struct Plan {
     int64_t items;
-    int tiles, splits;
+    int waves;  // of the tiles kernel; 0: the rows kernel
+    int tile_pairs, tiles, splits;
     int64_t part_bytes, bytes;
 };
 
 // False for sizes out of range.
-bool plan_of(const spconv_batch *B, int q_heads, int heads, int dim, int keep, Plan *p) {
+bool plan_of(int dtype, const spconv_batch *B, int q_heads, int heads, int dim, int keep, Plan *p) {
     const int group = q_heads / heads;
-    p->tiles = (B->q_block * group + 15) / 16;
+    const int64_t pairs = (int64_t)B->q_block * group;
+    p->waves = 0;
+    p->tile_pairs = 16;
+    if (pairs > 16) {
+        const int most = dtype == SPCONV_F32 || dim > 128 ? 4 : 8;  // registers of the wider ones
+        p->waves = 2;
+        while (p->waves < most && p->waves * 32 < pairs) p->waves *= 2;
+        p->tile_pairs = p->waves * 32;
+    }
+    p->tiles = (int)((pairs + p->tile_pairs - 1) / p->tile_pairs);
     p->items = rows_of(B) * heads * p->tiles;
     if (p->items >= ((int64_t)1 << 27)) return false;
-    // Shares of a row's keys: enough workgroups for two on every CU, 256 keys (two turns of the waves) each at least.
+    // Shares of a row's keys: enough workgroups for two on every CU, 256 keys each at least.
     const int64_t keys = (int64_t)(keep ? keep : B->max_blocks) * B->block;
     int64_t splits = (512 + p->items - 1) / p->items;
     splits = std::min<int64_t>(splits, (keys + 255) / 256);
     p->splits = (int)std::max<int64_t>(1, splits);
     p->part_bytes = p->bytes = 0;
     if (p->splits > 1) {
-        p->part_bytes = p->items * p->splits * 16 * dim * 4;
-        p->bytes = p->part_bytes + p->items * p->splits * 16 * 2 * 4;
+        p->part_bytes = p->items * p->splits * p->tile_pairs * dim * 4;
+        p->bytes = p->part_bytes + p->items * p->splits * p->tile_pairs * 2 * 4;
     }
     return true;
 }
 
+template <typename T, int NK, int KT>
+void launch_tiles(const AttnArgs &a, int waves, dim3 grid, hipStream_t stream) {
+    if (waves == 2)
+        tiles_kernel<T, NK, KT, 128><<<grid, 128, 0, stream>>>(a);
+    else if (waves == 4)
+        tiles_kernel<T, NK, KT, 256><<<grid, 256, 0, stream>>>(a);
+    else if constexpr (sizeof(T) == 2 && NK <= 4)
+        tiles_kernel<T, NK, KT, 512><<<grid, 512, 0, stream>>>(a);
+}
+
 template <typename T>
-int attention_of(const AttnArgs &a, hipStream_t stream) {
+int attention_of(const AttnArgs &a, const Plan &p, hipStream_t stream) {
     const dim3 grid = grid_of(a.items * a.splits);
-    if (a.dim <= 64)
-        rows_kernel<T, 2><<<grid, 256, 0, stream>>>(a);
-    else if (a.dim <= 128)
-        rows_kernel<T, 4><<<grid, 256, 0, stream>>>(a);
-    else
-        rows_kernel<T, 8><<<grid, 256, 0, stream>>>(a);
+    if (p.waves == 0) {
+        if (a.dim <= 64)
+            rows_kernel<T, 2><<<grid, 256, 0, stream>>>(a);
+        else if (a.dim <= 128)
+            rows_kernel<T, 4><<<grid, 256, 0, stream>>>(a);
+        else
+            rows_kernel<T, 8><<<grid, 256, 0, stream>>>(a);
+    } else {
+        if (a.dim <= 64)
+            launch_tiles<T, 2, 64>(a, p.waves, grid, stream);
+        else if (a.dim <= 128)
+            launch_tiles<T, 4, 64>(a, p.waves, grid, stream);
+        else
+            launch_tiles<T, 8, sizeof(T) == 4 ? 32 : 64>(a, p.waves, grid, stream);
+    }
     if (hipGetLastError() != hipSuccess) return SPCONV_EHIP;
     if (a.splits > 1) {
-        join_kernel<T><<<grid_of(a.items * 16), 256, 0, stream>>>(a);
+        join_kernel<T><<<grid_of(a.items * a.tile_pairs), 256, 0, stream>>>(a);
         return launched();
     }
     return SPCONV_OK;
@@ -455,7 +886,7 @@ extern "C" int spconv_attention_workspace(int dtype, const spconv_batch *batch, 
                                           int64_t *bytes) {
     Plan p;
     if (!batch_ok(batch) || !dtype_ok(dtype) || !heads_ok(q_heads, heads, dim) || keep < 0 || bytes == nullptr ||
-        !plan_of(batch, q_heads, heads, dim, keep, &p))
+        !plan_of(dtype, batch, q_heads, heads, dim, keep, &p))
         return SPCONV_EINVAL;
     *bytes = p.bytes;
     return SPCONV_OK;
@@ -471,16 +902,17 @@ extern "C" int spconv_block_attention(int dtype, const spconv_batch *batch, cons
         q == nullptr || k_cache == nullptr || v_cache == nullptr || out == nullptr || q_token < 0 || q_head < 0 ||
         !out_strides_ok(batch->tokens, q_heads, dim, out_token, out_head) || !aligned16(k_cache) ||
         !aligned16(v_cache) || !std::isfinite(scale) || keep < 0 || (blocks == nullptr) != (keep == 0) ||
-        (counts != nullptr && blocks == nullptr) || !plan_of(batch, q_heads, heads, dim, keep, &p))
+        (counts != nullptr && blocks == nullptr) || !plan_of(dtype, batch, q_heads, heads, dim, keep, &p))
         return SPCONV_EINVAL;
     if (p.bytes > 0 && (workspace == nullptr || !aligned16(workspace) || workspace_bytes < p.bytes)) return SPCONV_EINVAL;
     AttnArgs a{*batch, q, q_token, q_head, k_cache, v_cache, blocks, counts, out, out_token, out_head, lse,
                (float *)workspace, nullptr, p.items, heads, q_heads / heads, dim, keep, p.tiles, p.splits,
-               rows_aligned16(q, q_token, q_head, size_of(dtype)), scale * kLog2e, make_div((uint32_t)p.tiles),
-               make_div((uint32_t)heads), make_div((uint32_t)(q_heads / heads)), make_div((uint32_t)p.splits),
-               make_div((uint32_t)(batch->block / 16))};
+               rows_aligned16(q, q_token, q_head, size_of(dtype)),
+               rows_aligned16(out, out_token, out_head, size_of(dtype)), p.tile_pairs, scale * kLog2e,
+               make_div((uint32_t)p.tiles), make_div((uint32_t)heads), make_div((uint32_t)(q_heads / heads)),
+               make_div((uint32_t)p.splits), make_div((uint32_t)(batch->block / 16)), make_div((uint32_t)p.tile_pairs)};
     if (p.bytes > 0) a.stat = (float *)((char *)workspace + p.part_bytes);
-    if (dtype == SPCONV_F32) return attention_of<float>(a, stream);
-    if (dtype == SPCONV_F16) return attention_of<_Float16>(a, stream);
-    return attention_of<__bf16>(a, stream);
+    if (dtype == SPCONV_F32) return attention_of<float>(a, p, stream);
+    if (dtype == SPCONV_F16) return attention_of<_Float16>(a, p, stream);
+    return attention_of<__bf16>(a, p, stream);
 }
