@@ -112,7 +112,52 @@ __device__ __forceinline__ float log_sum(float ref, float sum) {
     return sum == 0.0f ? -kInf : (ref + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
-constexpr int kEntries = 256;  // list entries whose pages are looked up at a time
+// The keys that a tile may read, 16 at a time (slabs: a sixteenth of a page's rows or more lie
+// side by side): the first key of each and its place in the cache, looked up for kSlabs of them at a time.
+constexpr int kSlabs = 256;
+struct Slabs {
+    int key[kSlabs + 8];       // -1: nothing of it is seen
+    int64_t base[kSlabs + 8];  // elements
+};
+
+// Slabs [s0, s0 + kSlabs) of a row's list, those below s_hi; THREADS threads.
+template <int THREADS>
+__device__ __forceinline__ void look_up(Slabs &S, const AttnArgs &a, const Pairs &P, int64_t s0, int64_t s_hi) {
+    const spconv_batch &B = a.B;
+    const int spb = B.block >> 4;
+    const int e0 = (int)(s0 / spb), r0 = (int)(s0 - (int64_t)e0 * spb);
+    for (int i = threadIdx.x; i < kSlabs + 8; i += THREADS) {
+        int key = -1;
+        int64_t base = 0;
+        if (i < kSlabs && s0 + i < s_hi) {
+            const int de = (uint32_t)(r0 + i) / a.slab_div, sub = r0 + i - de * spb;
+            const int j = a.blocks ? a.blocks[P.rh * a.keep + e0 + de] : e0 + de;
+            if (j >= 0 && j < B.max_blocks && j <= P.last / B.block) {
+                const int page = page_of(B, P.r.b, j), k0 = j * B.block + sub * 16;
+                if (page >= 0 && k0 <= P.last) {
+                    key = k0;
+                    base = (((int64_t)page * a.heads + P.h) * B.block + sub * 16) * a.dim;
+                }
+            }
+        }
+        S.key[i] = key;
+        S.base[i] = base;
+    }
+}
+
+// Slabs of the row's list.
+__device__ __forceinline__ int64_t slabs_of(const AttnArgs &a, const Pairs &P) {
+    int entries = 0;
+    if (P.last >= 0)
+        entries = !a.blocks ? min(P.last / a.B.block + 1, a.B.max_blocks)
+                            : a.counts ? clamp_int(a.counts[P.rh], 0, a.keep) : a.keep;
+    return (int64_t)entries * (a.B.block >> 4);
+}
+
+__device__ __forceinline__ int64_t uniform64(int64_t x) {
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x), hi = __builtin_amdgcn_readfirstlane((uint32_t)(x >> 32));
+    return (int64_t)(((uint64_t)hi << 32) | lo);
+}
 
 __device__ __forceinline__ bool not_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u; }
 
@@ -127,7 +172,7 @@ __global__ __launch_bounds__(256) void rows_kernel(AttnArgs a) {
     constexpr int kJoin = 16 * (DP + 4) * 4;
     constexpr int kPerWave = kTile > kJoin ? kTile : kJoin;
     __shared__ __attribute__((aligned(16))) char lds[4 * kPerWave];
-    __shared__ int e_block[kEntries], e_page[kEntries];
+    __shared__ Slabs S;
     __shared__ float w_max[4][16], w_sum[4][16];
     typedef typename VecOf<T, W>::type V;
 
@@ -137,9 +182,8 @@ __global__ __launch_bounds__(256) void rows_kernel(AttnArgs a) {
     const int split = (int)((uint32_t)idx - item * a.split_div.d);
     const Pairs P = find_pairs(a, item);
     if (P.r.n == 0) return;
-    const spconv_batch &B = a.B;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, part = lane >> 4;
-    const int D = a.dim, spb = B.block >> 4;
+    const int D = a.dim;
 
     // Query of this lane's column.
     const int m = P.m0 + col, tok = (uint32_t)m / a.group_div;
@@ -163,11 +207,8 @@ __global__ __launch_bounds__(256) void rows_kernel(AttnArgs a) {
         }
     }
 
-    // This share of the row's slabs (16 keys of a block).
-    int entries = 0;
-    if (P.last >= 0) entries = min(P.last / B.block + 1, B.max_blocks);
-    if (a.blocks) entries = P.last < 0 ? 0 : a.counts ? clamp_int(a.counts[P.rh], 0, a.keep) : a.keep;
-    const int64_t slabs = (int64_t)entries * spb;
+    // This share of the row's slabs.
+    const int64_t slabs = slabs_of(a, P);
     const int64_t per = ((slabs + 1) / 2 + a.splits - 1) / a.splits * 2;
     const int64_t s_lo = min(per * split, slabs), s_hi = min(s_lo + per, slabs);
     const int first_pos = P.r.p0 + (int)((uint32_t)P.m0 / a.group_div);  // position of the tile's first token
@@ -179,37 +220,20 @@ __global__ __launch_bounds__(256) void rows_kernel(AttnArgs a) {
     float top = -kInf, sum = 0.0f;
     T *vt = reinterpret_cast<T *>(lds + wave * kPerWave);
 
-    for (int e0 = s_lo < s_hi ? (int)(s_lo / spb) : 0; (int64_t)e0 * spb < s_hi; e0 += kEntries) {
+    for (int64_t c0 = s_lo; c0 < s_hi; c0 += kSlabs) {
         __syncthreads();
-        {
-            const int e = e0 + tid;
-            int j = -1, page = -1;
-            if (e < entries) {
-                j = a.blocks ? a.blocks[P.rh * a.keep + e] : e;
-                if (j >= 0 && j <= P.last / B.block && j < B.max_blocks) page = page_of(B, P.r.b, j);
-            }
-            e_block[tid] = j;
-            e_page[tid] = page;
-        }
+        look_up<256>(S, a, P, c0, s_hi);
         __syncthreads();
-        const int lo = (int)(max(s_lo, (int64_t)e0 * spb) - (int64_t)e0 * spb);
-        const int hi = (int)(min(s_hi, ((int64_t)e0 + kEntries) * spb) - (int64_t)e0 * spb);
-        for (int s = lo + 2 * wave; s < hi; s += 8) {
+        const int n_slabs = (int)min(s_hi - c0, (int64_t)kSlabs);
+        for (int s = 2 * wave; s < n_slabs; s += 8) {
             int key0[2];
             int64_t base[2];
             bool there[2];
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-                const int e = (uint32_t)(s + t) / a.slab_div, sub = (s + t) - e * spb;
-                there[t] = false;
-                key0[t] = 0;
-                base[t] = 0;
-                if (s + t < hi) {
-                    const int page = __builtin_amdgcn_readfirstlane(e_page[e]);
-                    key0[t] = __builtin_amdgcn_readfirstlane(e_block[e]) * B.block + sub * 16;
-                    there[t] = page >= 0 && key0[t] <= P.last;
-                    base[t] = (((int64_t)page * a.heads + P.h) * B.block + sub * 16) * D;
-                }
+                key0[t] = __builtin_amdgcn_readfirstlane(S.key[s + t]);
+                base[t] = uniform64(S.base[s + t]);
+                there[t] = key0[t] >= 0;
             }
             if (!there[0] && !there[1]) continue;
             // Keys: rows of the first product straight from memory.
@@ -383,6 +407,7 @@ __global__ __launch_bounds__(256) void rows_kernel(AttnArgs a) {
 // ---- many pairs: 32x32 tiles, keys and values staged in LDS for all waves ----
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ f32x16 mma32(frag_t<__bf16> a, frag_t<__bf16> b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
@@ -430,12 +455,12 @@ __device__ __forceinline__ int value_unit(int r, int c) {
 // to 2^8 are as exact as those up to 1, and the output is rescaled a few times a row instead of
 // nearly every tile.
 template <typename T, int NK, int KT, int THREADS>
-__global__ __launch_bounds__(THREADS) void tiles_kernel(AttnArgs a) {
+__global__ __launch_bounds__(THREADS, NK <= 4 && sizeof(T) == 2 ? 2 : 1) void tiles_kernel(AttnArgs a) {
     constexpr int DP = NK * 32, W = kPer16<T>, UPR = DP / W, SIZE = (int)sizeof(T);
     constexpr int NL = KT * UPR / THREADS;  // units a thread stages of a tile's keys, and of its values
     constexpr int NS = KT / 16, NB = KT / 32, NQ = DP / 16, NT = DP / 32;
     __shared__ __attribute__((aligned(16))) T lds[2][2][KT * DP];
-    __shared__ int e_block[kEntries], e_page[kEntries];
+    __shared__ Slabs S;
     typedef typename VecOf<T, W>::type V;
     typedef typename VecOf<T, 4>::type V4;
 
@@ -447,9 +472,9 @@ __global__ __launch_bounds__(THREADS) void tiles_kernel(AttnArgs a) {
     const int split = (int)((uint32_t)idx - item * a.split_div.d);
     const Pairs P = find_pairs(a, item);
     if (P.r.n == 0) return;
-    const spconv_batch &B = a.B;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 31, half = lane >> 5;
-    const int D = a.dim, spb = B.block >> 4;
+    const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, half = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int D = a.dim;
 
     // Query of this lane's column. The sign of the scale goes into it.
     const int m = P.m0 + wave * 32 + col, tok = (uint32_t)m / a.group_div;
@@ -481,10 +506,7 @@ __global__ __launch_bounds__(THREADS) void tiles_kernel(AttnArgs a) {
     const int wave_first = P.r.p0 + (int)((uint32_t)w0 / a.group_div);
     const int wave_last = w0 < P.end ? P.r.p0 + (int)((uint32_t)(min(w0 + 32, P.end) - 1) / a.group_div) : -1;
 
-    int entries = 0;
-    if (P.last >= 0) entries = min(P.last / B.block + 1, B.max_blocks);
-    if (a.blocks) entries = P.last < 0 ? 0 : a.counts ? clamp_int(a.counts[P.rh], 0, a.keep) : a.keep;
-    const int64_t slabs = (int64_t)entries * spb;
+    const int64_t slabs = slabs_of(a, P);
     const int64_t per = ((slabs + NS - 1) / NS + a.splits - 1) / a.splits * NS;
     const int64_t s_lo = min(per * split, slabs), s_hi = min(s_lo + per, slabs);
 
@@ -495,78 +517,68 @@ __global__ __launch_bounds__(THREADS) void tiles_kernel(AttnArgs a) {
         for (int i = 0; i < 16; ++i) o[t][i] = 0.0f;
     float top = -kInf, sum = 0.0f;  // top: of the products before scaling
 
-    for (int e0 = s_lo < s_hi ? (int)(s_lo / spb) : 0; (int64_t)e0 * spb < s_hi; e0 += kEntries) {
-        __syncthreads();
-        for (int i = tid; i < kEntries; i += THREADS) {
-            const int e = e0 + i;
-            int j = -1, page = -1;
-            if (e < entries) {
-                j = a.blocks ? a.blocks[P.rh * a.keep + e] : e;
-                if (j >= 0 && j <= P.last / B.block && j < B.max_blocks) page = page_of(B, P.r.b, j);
-            }
-            e_block[i] = j;
-            e_page[i] = page;
-        }
-        __syncthreads();
-        const int lo = (int)(max(s_lo, (int64_t)e0 * spb) - (int64_t)e0 * spb);
-        const int hi = (int)(min(s_hi, ((int64_t)e0 + kEntries) * spb) - (int64_t)e0 * spb);
+    // What this thread stages of a tile: unit (lane % UPR) of rows lane / UPR from its wave's first
+    // ones on; a wave's units of one turn lie in one slab.
+    const int my_row = lane / UPR, my_unit = lane % UPR;
+    const bool my = my_unit * W < D;
+    const uint32_t my_at = my ? (uint32_t)(my_row * D + my_unit * W) : 0u;
+    if (D < DP) {  // components behind the last one stay zero
+        for (int i = tid; i < 4 * KT * DP / W; i += THREADS) reinterpret_cast<u32x4 *>(&lds[0][0][0])[i] = u32x4{0, 0, 0, 0};
+    }
 
-        // First key of slab s and its place in the cache; -1 where nothing of it is seen.
-        auto slab = [&](int s, int64_t &base) {
-            base = 0;
-            if (s >= hi) return -1;
-            const int e = (uint32_t)s / a.slab_div, sub = s - e * spb;
-            const int page = __builtin_amdgcn_readfirstlane(e_page[e]);
-            const int key0 = __builtin_amdgcn_readfirstlane(e_block[e]) * B.block + sub * 16;
-            base = (((int64_t)page * a.heads + P.h) * B.block + sub * 16) * D;
-            return page >= 0 && key0 <= P.last ? key0 : -1;
-        };
+    for (int64_t c0 = s_lo; c0 < s_hi; c0 += kSlabs) {
+        __syncthreads();
+        look_up<THREADS>(S, a, P, c0, s_hi);
+        __syncthreads();
+        const int n_slabs = (int)min(s_hi - c0, (int64_t)kSlabs);
+
         V kr[NL], vr[NL];
+        int next[NS];  // first keys of the fetched tile's slabs
+        // (Of slabs that are not there the first page's rows are read, and masked or zeroed below.)
         auto fetch = [&](int s0) {
 #pragma unroll
-            for (int i = 0; i < NL; ++i) {
-                const int row = (i * THREADS + wave * 64) / UPR + lane / UPR, c = lane % UPR;
-                int64_t base;
-                const int key0 = slab(s0 + (i * THREADS + wave * 64) / UPR / 16, base);
+            for (int n = 0; n < NS; ++n) next[n] = __builtin_amdgcn_readfirstlane(S.key[s0 + n]);
 #pragma unroll
-                for (int e = 0; e < W; ++e) kr[i][e] = vr[i][e] = (T)0.0f;
-                if (key0 >= 0 && c * W < D) {
-                    const int64_t at = base + (row & 15) * D + c * W;
-                    kr[i] = *reinterpret_cast<const V *>((const T *)a.k_cache + at);
-                    // Values that no pair sees stay zero, whatever lies there: their weights
-                    // are zero, and zero times infinity is not.
-                    if (key0 + (row & 15) <= P.last) vr[i] = *reinterpret_cast<const V *>((const T *)a.v_cache + at);
-                }
+            for (int i = 0; i < NL; ++i) {
+                const int row0 = (i * THREADS + wave * 64) / UPR;
+                const int64_t base = uniform64(S.base[s0 + row0 / 16]) + (row0 & 15) * D;
+                kr[i] = *reinterpret_cast<const V *>((const T *)a.k_cache + base + my_at);
+                vr[i] = *reinterpret_cast<const V *>((const T *)a.v_cache + base + my_at);
             }
         };
-        // Whether every pair of the workgroup sees the whole tile.
-        auto whole = [&](int s0) {
+        // Whether every pair of the workgroup sees the whole fetched tile.
+        auto whole = [&]() {
             bool w = true;
-            int64_t base;
 #pragma unroll
-            for (int n = 0; n < NS; ++n) {
-                const int key0 = slab(s0 + n, base);
-                w = w && key0 >= 0 && key0 + 15 <= first_pos;
-            }
+            for (int n = 0; n < NS; ++n) w = w && next[n] >= 0 && next[n] + 15 <= first_pos;
             return w;
         };
-        // The fetched tile into LDS. In a tile that some see a part of, values that are not finite are
-        // taken out (returns whether there are any); they come back in a pass of their own.
-        auto put = [&](int buf, bool full) {
+        // The fetched tile into LDS. Values that no pair sees become zero, whatever lies there: their weights
+        // are zero, and zero times infinity is not. In a tile that some see a part of, all values that
+        // are not finite are taken out (returns whether there are any); they come back in a pass of their own.
+        auto put = [&](int s0, int buf, bool full) {
             bool odd = false;
+            if (!full) {
+#pragma unroll
+                for (int i = 0; i < NL; ++i) {
+                    const int row0 = (i * THREADS + wave * 64) / UPR;
+                    const int k0 = S.key[s0 + row0 / 16];
+                    const bool seen = k0 >= 0 && k0 + (row0 & 15) + my_row <= P.last;
+#pragma unroll
+                    for (int e = 0; e < W; ++e) {
+                        const bool bad = not_finite((float)vr[i][e]);
+                        odd = odd || (seen && bad);
+                        if (!seen || bad) vr[i][e] = (T)0.0f;
+                    }
+                }
+            }
 #pragma unroll
             for (int i = 0; i < NL; ++i) {
-                const int row = (i * THREADS + wave * 64) / UPR + lane / UPR, c = lane % UPR;
-                if (!full) {
-#pragma unroll
-                    for (int e = 0; e < W; ++e)
-                        if (not_finite((float)vr[i][e])) {
-                            odd = true;
-                            vr[i][e] = (T)0.0f;
-                        }
+                const int row = (i * THREADS + wave * 64) / UPR + my_row;
+                if (my) {
+                    *reinterpret_cast<V *>(&lds[buf][0][row * DP + key_unit<UPR>(row, my_unit) * W]) = kr[i];
+                    *reinterpret_cast<V *>(&lds[buf][1][row * DP + value_unit<UPR, SIZE>(row, my_unit) * W]) = vr[i];
                 }
-                *reinterpret_cast<V *>(&lds[buf][0][row * DP + key_unit<UPR>(row, c) * W]) = kr[i];
-                *reinterpret_cast<V *>(&lds[buf][1][row * DP + value_unit<UPR, SIZE>(row, c) * W]) = vr[i];
             }
             return odd;
         };
@@ -595,33 +607,34 @@ __global__ __launch_bounds__(THREADS) void tiles_kernel(AttnArgs a) {
             return f;
         };
 
-        fetch(lo);
-        bool full = whole(lo);
-        bool odd = put(0, full);
+        fetch(0);
+        bool full = whole();
+        bool odd = put(0, 0, full);
         if (full)
             __syncthreads();
         else
             odd = __syncthreads_or(odd);
         int buf = 0;
-        for (int s0 = lo; s0 < hi; s0 += NS, buf ^= 1) {
-            const bool more = s0 + NS < hi;
-            if (more) fetch(s0 + NS);
+        for (int s0 = 0; s0 < n_slabs; s0 += NS, buf ^= 1) {
+            const bool more = s0 + NS < n_slabs;
             int key0[NS], low = 0x7fffffff;
-            int64_t base;
 #pragma unroll
             for (int n = 0; n < NS; ++n) {
-                key0[n] = slab(s0 + n, base);
+                key0[n] = next[n];
                 if (key0[n] >= 0) low = min(low, key0[n]);
             }
+            if (more) fetch(s0 + NS);
             const T *ks = lds[buf][0], *vs = lds[buf][1];
             if (low <= wave_last) {
                 f32x16 x[NB];
 #pragma unroll
-                for (int b = 0; b < NB; ++b) {
+                for (int b = 0; b < NB; ++b)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) x[b][i] = 0.0f;
 #pragma unroll
-                    for (int k = 0; k < NQ; ++k) {
+                for (int k = 0; k < NQ; ++k)
+#pragma unroll
+                    for (int b = 0; b < NB; ++b) {
                         const int r = b * 32 + col;
                         frag_t<T> f;
                         if constexpr (SIZE == 2) {
@@ -637,7 +650,6 @@ __global__ __launch_bounds__(THREADS) void tiles_kernel(AttnArgs a) {
                         }
                         x[b] = mma32(f, q[k], x[b]);
                     }
-                }
                 bool cut = !full;
                 if (cut) {  // this wave may see all of it
                     cut = false;
@@ -685,7 +697,7 @@ __global__ __launch_bounds__(THREADS) void tiles_kernel(AttnArgs a) {
                 }
                 sum += (total[0] + total[1]) + (total[2] + total[3]);
             }
-            if (odd) {
+            if (__builtin_expect(odd, 0)) {
                 // Values that are not finite, where some see a part of the tile only: products of
                 // who sees a key (1 or 0) with where its value is +infinity or NaN, then
                 // -infinity or NaN, say which outputs take part.
@@ -693,20 +705,21 @@ __global__ __launch_bounds__(THREADS) void tiles_kernel(AttnArgs a) {
                     __syncthreads();
 #pragma unroll
                     for (int i = 0; i < NL; ++i) {
-                        const int row = (i * THREADS + wave * 64) / UPR + lane / UPR, c = lane % UPR;
-                        const int k0 = slab(s0 + (i * THREADS + wave * 64) / UPR / 16, base);
+                        const int row0 = (i * THREADS + wave * 64) / UPR, row = row0 + my_row;
+                        const int k0 = S.key[s0 + row0 / 16];
                         V v;
 #pragma unroll
                         for (int e = 0; e < W; ++e) v[e] = (T)0.0f;
-                        if (k0 >= 0 && k0 + (row & 15) <= P.last && c * W < D) {
-                            const V x = *reinterpret_cast<const V *>((const T *)a.v_cache + base + (row & 15) * D + c * W);
+                        if (k0 >= 0 && k0 + (row & 15) <= P.last && my) {
+                            const int64_t base = uniform64(S.base[s0 + row0 / 16]) + (row0 & 15) * D;
+                            const V x = *reinterpret_cast<const V *>((const T *)a.v_cache + base + my_at);
 #pragma unroll
                             for (int e = 0; e < W; ++e) {
                                 const float f = (float)x[e];
                                 v[e] = (T)(f != f || f == (sign ? -kInf : kInf) ? 1.0f : 0.0f);
                             }
                         }
-                        *reinterpret_cast<V *>(&lds[buf][1][row * DP + value_unit<UPR, SIZE>(row, c) * W]) = v;
+                        *reinterpret_cast<V *>(&lds[buf][1][row * DP + value_unit<UPR, SIZE>(row, my_unit) * W]) = v;
                     }
                     __syncthreads();
 #pragma unroll
@@ -731,8 +744,8 @@ __global__ __launch_bounds__(THREADS) void tiles_kernel(AttnArgs a) {
                 }
             }
             if (more) {
-                full = whole(s0 + NS);
-                odd = put(buf ^ 1, full);
+                full = whole();
+                odd = put(s0 + NS, buf ^ 1, full);
                 if (full)
                     __syncthreads();
                 else
@@ -868,9 +881,9 @@ int attention_of(const AttnArgs &a, const Plan &p, hipStream_t stream) {
         if (a.dim <= 64)
             launch_tiles<T, 2, 64>(a, p.waves, grid, stream);
         else if (a.dim <= 128)
-            launch_tiles<T, 4, 64>(a, p.waves, grid, stream);
+            launch_tiles<T, 4, sizeof(T) == 4 ? 32 : 64>(a, p.waves, grid, stream);
         else
-            launch_tiles<T, 8, sizeof(T) == 4 ? 32 : 64>(a, p.waves, grid, stream);
+            launch_tiles<T, 8, 32>(a, p.waves, grid, stream);
     }
     if (hipGetLastError() != hipSuccess) return SPCONV_EHIP;
     if (a.splits > 1) {
