@@ -13,6 +13,8 @@
 // in which the weights came out (slot 8*(l/16) + 4*t + i of lane l is key 16*t + 4*(l/16) + i).
 #include "batch.h"
 
+#include <type_traits>
+
 namespace {
 
 constexpr float kInf = __builtin_huge_valf();
@@ -116,17 +118,19 @@ __device__ __forceinline__ float log_sum(float ref, float sum) {
 // side by side): the first key of each and its place in the cache, looked up for kSlabs of them at a time.
 constexpr int kSlabs = 256;
 struct Slabs {
-    int key[kSlabs + 8];       // -1: nothing of it is seen
-    int64_t base[kSlabs + 8];  // elements
+    int64_t base[kSlabs + 16];  // elements; 0 behind the last
+    int key[kSlabs + 16];       // -1: nothing of it is seen
+    uint64_t part[kSlabs / 64]; // a bit for each slab: not all of it is seen by every pair
 };
 
-// Slabs [s0, s0 + kSlabs) of a row's list, those below s_hi; THREADS threads.
+// Slabs [s0, s0 + kSlabs) of a row's list, those below s_hi; THREADS threads. first_pos: the first pair's position.
 template <int THREADS>
-__device__ __forceinline__ void look_up(Slabs &S, const AttnArgs &a, const Pairs &P, int64_t s0, int64_t s_hi) {
+__device__ __forceinline__ void look_up(Slabs &S, const AttnArgs &a, const Pairs &P, int64_t s0, int64_t s_hi,
+                                        int first_pos) {
     const spconv_batch &B = a.B;
     const int spb = B.block >> 4;
     const int e0 = (int)(s0 / spb), r0 = (int)(s0 - (int64_t)e0 * spb);
-    for (int i = threadIdx.x; i < kSlabs + 8; i += THREADS) {
+    for (int i = threadIdx.x; i < kSlabs + 64; i += THREADS) {  // whole waves
         int key = -1;
         int64_t base = 0;
         if (i < kSlabs && s0 + i < s_hi) {
@@ -140,8 +144,12 @@ __device__ __forceinline__ void look_up(Slabs &S, const AttnArgs &a, const Pairs
                 }
             }
         }
-        S.key[i] = key;
-        S.base[i] = base;
+        if (i < kSlabs + 16) {
+            S.key[i] = key;
+            S.base[i] = base;
+        }
+        const uint64_t part = __ballot(key < 0 || key + 15 > first_pos);
+        if ((threadIdx.x & 63) == 0 && i < kSlabs) S.part[i >> 6] = part;
     }
 }
 
@@ -222,7 +230,7 @@ __global__ __launch_bounds__(256) void rows_kernel(AttnArgs a) {
 
     for (int64_t c0 = s_lo; c0 < s_hi; c0 += kSlabs) {
         __syncthreads();
-        look_up<256>(S, a, P, c0, s_hi);
+        look_up<256>(S, a, P, c0, s_hi, first_pos);
         __syncthreads();
         const int n_slabs = (int)min(s_hi - c0, (int64_t)kSlabs);
         for (int s = 2 * wave; s < n_slabs; s += 8) {
@@ -421,6 +429,19 @@ __device__ __forceinline__ f32x16 mma32(frag_t<float> a, frag_t<float> b, f32x16
     return c;
 }
 
+// x, as a value that the compiler knows nothing about: what is derived from it is formed where it
+// is used, and not kept in registers through the loops before.
+__device__ __forceinline__ int fresh(int x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
+// x, formed where this stands.
+__device__ __forceinline__ float settled(float x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
 // Max and sum over the two lanes that hold one column (lanes l, l+32).
 __device__ __forceinline__ float half_max(float x) {
     const uint32_t u = __float_as_uint(x);
@@ -461,6 +482,7 @@ __global__ __launch_bounds__(THREADS, NK <= 4 && sizeof(T) == 2 ? 2 : 1) void ti
     constexpr int NS = KT / 16, NB = KT / 32, NQ = DP / 16, NT = DP / 32;
     __shared__ __attribute__((aligned(16))) T lds[2][2][KT * DP];
     __shared__ Slabs S;
+    __shared__ int any_odd;
     typedef typename VecOf<T, W>::type V;
     typedef typename VecOf<T, 4>::type V4;
 
@@ -501,10 +523,7 @@ __global__ __launch_bounds__(THREADS, NK <= 4 && sizeof(T) == 2 ? 2 : 1) void ti
         }
     }
     const int first_pos = P.r.p0 + (int)((uint32_t)P.m0 / a.group_div);
-    // Of this wave's pairs: the first and last positions.
-    const int w0 = P.m0 + wave * 32;
-    const int wave_first = P.r.p0 + (int)((uint32_t)w0 / a.group_div);
-    const int wave_last = w0 < P.end ? P.r.p0 + (int)((uint32_t)(min(w0 + 32, P.end) - 1) / a.group_div) : -1;
+    const bool busy = P.m0 + wave * 32 < P.end;
 
     const int64_t slabs = slabs_of(a, P);
     const int64_t per = ((slabs + NS - 1) / NS + a.splits - 1) / a.splits * NS;
@@ -517,73 +536,105 @@ __global__ __launch_bounds__(THREADS, NK <= 4 && sizeof(T) == 2 ? 2 : 1) void ti
         for (int i = 0; i < 16; ++i) o[t][i] = 0.0f;
     float top = -kInf, sum = 0.0f;  // top: of the products before scaling
 
+    constexpr bool two = THREADS == 512;  // two waves a SIMD
+    const bool late = wave >= 4;
+    f32x16 x[NB];      // products of a tile, keys by pairs
+    frag_t<T> w[NS];   // weights of a tile
+    auto phase_end = [&]() {
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+        __builtin_amdgcn_sched_barrier(0);
+    };
+
     // What this thread stages of a tile: unit (lane % UPR) of rows lane / UPR from its wave's first
     // ones on; a wave's units of one turn lie in one slab.
     const int my_row = lane / UPR, my_unit = lane % UPR;
     const bool my = my_unit * W < D;
     const uint32_t my_at = my ? (uint32_t)(my_row * D + my_unit * W) : 0u;
-    if (D < DP) {  // components behind the last one stay zero
-        for (int i = tid; i < 4 * KT * DP / W; i += THREADS) reinterpret_cast<u32x4 *>(&lds[0][0][0])[i] = u32x4{0, 0, 0, 0};
-    }
 
     for (int64_t c0 = s_lo; c0 < s_hi; c0 += kSlabs) {
         __syncthreads();
-        look_up<THREADS>(S, a, P, c0, s_hi);
+        look_up<THREADS>(S, a, P, c0, s_hi, first_pos);
+        if (tid == 0) any_odd = 0;
         __syncthreads();
         const int n_slabs = (int)min(s_hi - c0, (int64_t)kSlabs);
-
-        V kr[NL], vr[NL];
-        int next[NS];  // first keys of the fetched tile's slabs
-        // (Of slabs that are not there the first page's rows are read, and masked or zeroed below.)
-        auto fetch = [&](int s0) {
+        bool odd = false;
+        // Slabs that some pair does not see all of, a bit each.
+        uint64_t part[kSlabs / 64];
 #pragma unroll
-            for (int n = 0; n < NS; ++n) next[n] = __builtin_amdgcn_readfirstlane(S.key[s0 + n]);
+        for (int i = 0; i < kSlabs / 64; ++i) part[i] = (uint64_t)uniform64((int64_t)S.part[i]);
+        auto partial = [&](int t) {
+            const int s = t * NS;
+            const uint64_t lo = s & 64 ? part[1] : part[0], hi = s & 64 ? part[3] : part[2];
+            return (((s & 128 ? hi : lo) >> (s & 63)) & ((1u << NS) - 1)) != 0;
+        };
+        auto keys_of = [&](int t, int (&k)[NS]) {
+#pragma unroll
+            for (int n = 0; n < NS; ++n) k[n] = __builtin_amdgcn_readfirstlane(S.key[t * NS + n]);
+        };
+        V kr[NL], vr[NL];
+        // Where this thread's rows of a tile lie. (Of slabs that are not there the first page's rows are read, and
+        // masked or zeroed below.)
+        struct Places {
+            int64_t at[NL];
+        };
+        auto places = [&](int t) {
+            Places p;
+#pragma unroll
+            for (int i = 0; i < NL; ++i) p.at[i] = S.base[t * NS + (i * THREADS + wave * 64) / UPR / 16];
+            return p;
+        };
+        auto fetch = [&](V (&r)[NL], const void *cache, const Places &p) {
 #pragma unroll
             for (int i = 0; i < NL; ++i) {
                 const int row0 = (i * THREADS + wave * 64) / UPR;
-                const int64_t base = uniform64(S.base[s0 + row0 / 16]) + (row0 & 15) * D;
-                kr[i] = *reinterpret_cast<const V *>((const T *)a.k_cache + base + my_at);
-                vr[i] = *reinterpret_cast<const V *>((const T *)a.v_cache + base + my_at);
+                r[i] = *reinterpret_cast<const V *>((const T *)cache + p.at[i] + ((row0 & 15) * D + my_at));
             }
         };
-        // Whether every pair of the workgroup sees the whole fetched tile.
-        auto whole = [&]() {
-            bool w = true;
-#pragma unroll
-            for (int n = 0; n < NS; ++n) w = w && next[n] >= 0 && next[n] + 15 <= first_pos;
-            return w;
-        };
-        // The fetched tile into LDS. Values that no pair sees become zero, whatever lies there: their weights
-        // are zero, and zero times infinity is not. In a tile that some see a part of, all values that
-        // are not finite are taken out (returns whether there are any); they come back in a pass of their own.
-        auto put = [&](int s0, int buf, bool full) {
-            bool odd = false;
-            if (!full) {
-#pragma unroll
-                for (int i = 0; i < NL; ++i) {
-                    const int row0 = (i * THREADS + wave * 64) / UPR;
-                    const int k0 = S.key[s0 + row0 / 16];
-                    const bool seen = k0 >= 0 && k0 + (row0 & 15) + my_row <= P.last;
-#pragma unroll
-                    for (int e = 0; e < W; ++e) {
-                        const bool bad = not_finite((float)vr[i][e]);
-                        odd = odd || (seen && bad);
-                        if (!seen || bad) vr[i][e] = (T)0.0f;
-                    }
-                }
-            }
+        auto put_keys = [&](int t) {
 #pragma unroll
             for (int i = 0; i < NL; ++i) {
                 const int row = (i * THREADS + wave * 64) / UPR + my_row;
-                if (my) {
-                    *reinterpret_cast<V *>(&lds[buf][0][row * DP + key_unit<UPR>(row, my_unit) * W]) = kr[i];
-                    *reinterpret_cast<V *>(&lds[buf][1][row * DP + value_unit<UPR, SIZE>(row, my_unit) * W]) = vr[i];
-                }
+                u32x4 v = __builtin_bit_cast(u32x4, kr[i]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = my ? v[e] : 0u;  // components behind the last one are zero
+                *reinterpret_cast<u32x4 *>(&lds[0][t & 1][row * DP + key_unit<UPR>(row, my_unit) * W]) = v;
             }
-            return odd;
+        };
+        auto put_values = [&](int t) {
+#pragma unroll
+            for (int i = 0; i < NL; ++i) {
+                const int row = (i * THREADS + wave * 64) / UPR + my_row;
+                *reinterpret_cast<V *>(&lds[1][t & 1][row * DP + value_unit<UPR, SIZE>(row, my_unit) * W]) = vr[i];
+            }
+        };
+        // Of a tile that some pairs do not see all of: values that no pair sees become zero, whatever lies there
+        // (their weights are zero, and zero times infinity is not), and all others that are not finite too;
+        // those come back in a pass of their own. Each thread for what it has put there.
+        auto clean_values = [&](int t) {
+            const int ln = fresh(lane), my_row = ln / UPR, my_unit = ln % UPR;
+            if (my_unit * W >= D) return;
+#pragma unroll 1
+            for (int i = 0; i < NL; ++i) {
+                const int row0 = (i * THREADS + wave * 64) / UPR, row = row0 + my_row;
+                const int k0 = S.key[t * NS + row0 / 16];
+                const bool seen = k0 >= 0 && k0 + (row & 15) <= P.last;
+                V *at = reinterpret_cast<V *>(&lds[1][t & 1][row * DP + value_unit<UPR, SIZE>(row, my_unit) * W]);
+                V v = *at;
+#pragma unroll
+                for (int e = 0; e < W; ++e) {
+                    const bool bad = not_finite((float)v[e]);
+                    odd = odd || (seen && bad);
+                    if (!seen || bad) v[e] = (T)0.0f;
+                }
+                *at = v;
+            }
         };
         // Eight keys of values, as rows of the second product: components t*32 + col, slots of step n.
-        auto value_frag = [&](const T *v, int t, int n) {
+        auto value_frag = [&](const T *v, int t, int n, int lane) {
+            const int half = lane >> 5, col = lane & 31;
             frag_t<T> f;
             if constexpr (SIZE == 2) {
                 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -607,121 +658,192 @@ __global__ __launch_bounds__(THREADS, NK <= 4 && sizeof(T) == 2 ? 2 : 1) void ti
             return f;
         };
 
-        fetch(0);
-        bool full = whole();
-        bool odd = put(0, 0, full);
-        if (full)
-            __syncthreads();
-        else
-            odd = __syncthreads_or(odd);
-        int buf = 0;
-        for (int s0 = 0; s0 < n_slabs; s0 += NS, buf ^= 1) {
-            const bool more = s0 + NS < n_slabs;
-            int key0[NS], low = 0x7fffffff;
-#pragma unroll
-            for (int n = 0; n < NS; ++n) {
-                key0[n] = next[n];
-                if (key0[n] >= 0) low = min(low, key0[n]);
+        // Eight components of keys, as rows of the first product: keys b*32 + col, components k*16 + half*8 and on.
+        auto key_frag = [&](const T *ks, int b, int k) {
+            const int r = b * 32 + col;
+            if constexpr (SIZE == 2) {
+                return *reinterpret_cast<const frag_t<T> *>(ks + r * DP + key_unit<UPR>(r, k * 2 + half) * W);
+            } else {
+                union {
+                    V h[2];
+                    frag_t<T> f;
+                } u;
+                u.h[0] = *reinterpret_cast<const V *>(ks + r * DP + key_unit<UPR>(r, k * 4 + half * 2) * W);
+                u.h[1] = *reinterpret_cast<const V *>(ks + r * DP + key_unit<UPR>(r, k * 4 + half * 2 + 1) * W);
+                return u.f;
             }
-            if (more) fetch(s0 + NS);
-            const T *ks = lds[buf][0], *vs = lds[buf][1];
-            if (low <= wave_last) {
-                f32x16 x[NB];
+        };
+        // O^T += V^T P^T of tile t, if any, then S^T = K Q^T of tile t + 1. LDS reads run kLead matrix instructions
+        // ahead of those that they feed.
+        auto multiply = [&](auto with_outputs, int t) {
+            constexpr int kOut = decltype(with_outputs)::value ? NS * NT : 0, kAll = kOut + NQ * NB, kLead = 4;
+            const T *vs = lds[1][t & 1], *ks = lds[0][(t + 1) & 1];
+            frag_t<T> f[kLead];
+            auto read = [&](int i) {
+                return i < kOut ? value_frag(vs, i % NT, i / NT, lane) : key_frag(ks, (i - kOut) % NB, (i - kOut) / NB);
+            };
 #pragma unroll
-                for (int b = 0; b < NB; ++b)
+            for (int i = 0; i < kLead; ++i) f[i] = read(i);
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) x[b][i] = 0.0f;
+            for (int i = 0; i < kAll; ++i) {
+                if (i < kOut) {
+                    o[i % NT] = mma32(f[i % kLead], w[i / NT], o[i % NT]);
+                } else {
+                    const int b = (i - kOut) % NB, k = (i - kOut) / NB;
+                    f32x16 c = x[b];
+                    if (k == 0) {
 #pragma unroll
-                for (int k = 0; k < NQ; ++k)
-#pragma unroll
-                    for (int b = 0; b < NB; ++b) {
-                        const int r = b * 32 + col;
-                        frag_t<T> f;
-                        if constexpr (SIZE == 2) {
-                            f = *reinterpret_cast<const frag_t<T> *>(ks + r * DP + key_unit<UPR>(r, k * 2 + half) * W);
-                        } else {
-                            union {
-                                V h[2];
-                                frag_t<T> f;
-                            } u;
-                            u.h[0] = *reinterpret_cast<const V *>(ks + r * DP + key_unit<UPR>(r, k * 4 + half * 2) * W);
-                            u.h[1] = *reinterpret_cast<const V *>(ks + r * DP + key_unit<UPR>(r, k * 4 + half * 2 + 1) * W);
-                            f = u.f;
-                        }
-                        x[b] = mma32(f, q[k], x[b]);
+                        for (int e = 0; e < 16; ++e) c[e] = 0.0f;
                     }
-                bool cut = !full;
-                if (cut) {  // this wave may see all of it
-                    cut = false;
-#pragma unroll
-                    for (int n = 0; n < NS; ++n) cut = cut || key0[n] < 0 || key0[n] + 15 > wave_first;
+                    x[b] = mma32(f[i % kLead], q[k], c);
                 }
-                if (cut) {
+                if (i + kLead < kAll) f[i % kLead] = read(i + kLead);
+            }
+            if constexpr (SIZE == 2) {
+                // (Without this the compiler puts each read right before its use.)
+                constexpr int kFirst = kOut >= kLead ? 2 * kLead : kLead;
+                __builtin_amdgcn_sched_group_barrier(0x100, kFirst, 0);
 #pragma unroll
-                    for (int b = 0; b < NB; ++b)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const int k0 = key0[b * 2 + (i >> 3)], key = k0 + ((i >> 2) & 1) * 8 + half * 4 + (i & 3);
-                            x[b][i] = k0 >= 0 && key <= pos ? x[b][i] : -kInf;
-                        }
+                for (int i = 0; i < kAll; ++i) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                    if (i < 2 * NL) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);  // the next tile's loads
+                    if (i + kLead < kOut)
+                        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+                    else if (i + kLead < kAll)
+                        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
                 }
-                float hi32 = -kInf;
+            }
+        };
+        // Weights of tile t from its products.
+        auto weights = [&](int t) {
+            if (partial(t)) {
+                int key0[NS];
+                keys_of(t, key0);
 #pragma unroll
                 for (int b = 0; b < NB; ++b)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) hi32 = fmaxf(hi32, x[b][i]);
-                hi32 = half_max(hi32);
-                if (__ballot((hi32 - top) * scale2 > 8.0f)) {
-                    const float next = fmaxf(top, hi32);
-                    const float shrink = next == -kInf ? 1.0f : __builtin_amdgcn_exp2f((top - next) * scale2);
-                    top = next;
-                    sum *= shrink;
-#pragma unroll
-                    for (int t = 0; t < NT; ++t) o[t] *= shrink;
-                }
-                const float ref = top == -kInf ? 0.0f : -top * scale2;
-                float total[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                for (int b = 0; b < NB; ++b) {
-                    frag_t<T> w[2];
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        const float p = __builtin_amdgcn_exp2f(fmaf(x[b][i], scale2, ref));
-                        total[i & 3] += p;
-                        w[i >> 3][i & 7] = (T)p;
+                        const int k0 = key0[b * 2 + (i >> 3)], key = k0 + ((i >> 2) & 1) * 8 + half * 4 + (i & 3);
+                        x[b][i] = k0 >= 0 && key <= pos ? x[b][i] : -kInf;
                     }
-#pragma unroll
-                    for (int n = 0; n < 2; ++n)
-#pragma unroll
-                        for (int t = 0; t < NT; ++t) o[t] = mma32(value_frag(vs, t, b * 2 + n), w[n], o[t]);
-                }
-                sum += (total[0] + total[1]) + (total[2] + total[3]);
             }
-            if (__builtin_expect(odd, 0)) {
-                // Values that are not finite, where some see a part of the tile only: products of
-                // who sees a key (1 or 0) with where its value is +infinity or NaN, then
-                // -infinity or NaN, say which outputs take part.
-                for (int sign = 0; sign < 2; ++sign) {
-                    __syncthreads();
+            float hi4[4] = {-kInf, -kInf, -kInf, -kInf};
 #pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) hi4[(i >> 1) & 3] = fmaxf(hi4[(i >> 1) & 3], x[b][i]);
+            const float hi32 = half_max(fmaxf(fmaxf(hi4[0], hi4[1]), fmaxf(hi4[2], hi4[3])));
+            if (__ballot((hi32 - top) * scale2 > 8.0f)) {
+                const float up = fmaxf(top, hi32);
+                const float shrink = up == -kInf ? 1.0f : __builtin_amdgcn_exp2f((top - up) * scale2);
+                top = up;
+                sum *= shrink;
+#pragma unroll
+                for (int n = 0; n < NT; ++n) o[n] *= shrink;
+            }
+            const float ref = top == -kInf ? 0.0f : -top * scale2;
+            // (In steps of their own: the compiler would otherwise put each exponential behind
+            // its argument and before its sum, and wait for each.)
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[b][i] = fmaf(x[b][i], scale2, ref);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[b][i] = __builtin_amdgcn_exp2f(x[b][i]);
+            __builtin_amdgcn_sched_barrier(0);
+            float total[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    total[i & 3] += x[b][i];
+                    w[b * 2 + (i >> 3)][i & 7] = (T)x[b][i];
+                }
+            // (The sum is needed in the next tile only; formed there, it would keep all weights in registers.)
+            sum = settled(sum + ((total[0] + total[1]) + (total[2] + total[3])));
+        };
+
+        // Each tile takes a phase of matrix products (outputs of the tile before, products of this one) and
+        // one of exponentials. With eight waves two share a SIMD: the second four run a phase
+        // behind the first, so that the matrix unit and the vector unit of a SIMD are both busy; a barrier
+        // parts the phases (with four waves or less, other workgroups fill the gaps, and one barrier a
+        // tile is enough). Keys of tile t + 1 and values of tile t are put into LDS in the
+        // products' phase of tile t: at that time nobody reads those halves of the LDS any more, and
+        // their first reader comes a barrier later. The loads for the next such phase start there too.
+        const int tiles = (n_slabs + NS - 1) / NS;
+        auto stage = [&](int t, const Places &keys, const Places &values) {
+            put_keys(t + 1);
+            put_values(t);
+            fetch(kr, a.k_cache, keys);
+            fetch(vr, a.v_cache, values);
+        };
+        fetch(kr, a.k_cache, places(0));
+        fetch(vr, a.v_cache, places(0));
+        put_keys(0);
+        fetch(kr, a.k_cache, places(1));
+        __syncthreads();
+        if (two && late) phase_end();
+        stage(0, places(2), places(1));
+        if (partial(0)) clean_values(0);
+        // (The products behind the last tile are of what the LDS holds, and not used: a loop that
+        // is left in its middle makes the compiler copy the accumulators.)
+        if (busy) {
+            multiply(std::false_type{}, -1);
+            if (two) phase_end();
+            for (int t = 0; t < tiles; ++t) {
+                const Places keys = places(t + 3), values = places(t + 2);
+                weights(t);
+                phase_end();
+                stage(t + 1, keys, values);
+                multiply(std::true_type{}, t);
+                if (partial(t + 1)) clean_values(t + 1);
+                if (two) phase_end();
+            }
+        } else {
+            if (two) phase_end();
+            for (int t = 0; t < tiles; ++t) {
+                phase_end();
+                stage(t + 1, places(t + 3), places(t + 2));
+                if (partial(t + 1)) clean_values(t + 1);
+                if (two) phase_end();
+            }
+        }
+        if (two && !late) phase_end();
+        if (odd) any_odd = 1;
+        __syncthreads();
+        if (any_odd) {
+            // Values that are not finite, where some see a part of the tile only: products of
+            // who sees a key (1 or 0) with where its value is +infinity or NaN, then
+            // -infinity or NaN, say which outputs take part.
+            for (int u = 0; u < tiles; ++u) {
+                if (!partial(u)) continue;
+                int key0[NS];
+                keys_of(u, key0);
+                for (int sign = 0; sign < 2; ++sign) {
+                    const int ln = fresh(lane), my_row = ln / UPR, my_unit = ln % UPR;
+#pragma unroll 1
                     for (int i = 0; i < NL; ++i) {
                         const int row0 = (i * THREADS + wave * 64) / UPR, row = row0 + my_row;
-                        const int k0 = S.key[s0 + row0 / 16];
+                        const int k0 = S.key[u * NS + row0 / 16];
+                        const bool seen = k0 >= 0 && k0 + (row & 15) <= P.last && my_unit * W < D;
                         V v;
 #pragma unroll
                         for (int e = 0; e < W; ++e) v[e] = (T)0.0f;
-                        if (k0 >= 0 && k0 + (row & 15) <= P.last && my) {
-                            const int64_t base = uniform64(S.base[s0 + row0 / 16]) + (row0 & 15) * D;
-                            const V x = *reinterpret_cast<const V *>((const T *)a.v_cache + base + my_at);
+                        if (seen)
+                            v = *reinterpret_cast<const V *>((const T *)a.v_cache + S.base[u * NS + row0 / 16] +
+                                                             (row & 15) * D + my_unit * W);
 #pragma unroll
-                            for (int e = 0; e < W; ++e) {
-                                const float f = (float)x[e];
-                                v[e] = (T)(f != f || f == (sign ? -kInf : kInf) ? 1.0f : 0.0f);
-                            }
+                        for (int e = 0; e < W; ++e) {
+                            const float f = (float)v[e];
+                            v[e] = (T)(f != f || f == (sign ? -kInf : kInf) ? 1.0f : 0.0f);
                         }
-                        *reinterpret_cast<V *>(&lds[buf][1][row * DP + value_unit<UPR, SIZE>(row, my_unit) * W]) = v;
+                        *reinterpret_cast<V *>(&lds[1][0][row * DP + value_unit<UPR, SIZE>(row, my_unit) * W]) = v;
                     }
                     __syncthreads();
+                    const int p0 = fresh(pos) - (ln >> 5) * 4;
 #pragma unroll
                     for (int t = 0; t < NT; ++t) {
                         f32x16 hit;
@@ -729,40 +851,35 @@ __global__ __launch_bounds__(THREADS, NK <= 4 && sizeof(T) == 2 ? 2 : 1) void ti
                         for (int i = 0; i < 16; ++i) hit[i] = 0.0f;
 #pragma unroll
                         for (int n = 0; n < NS; ++n) {
-                            frag_t<T> w;
+                            frag_t<T> see;
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) {
-                                const int key = key0[n] + (i >> 2) * 8 + half * 4 + (i & 3);
-                                w[i] = (T)(key0[n] >= 0 && key <= pos ? 1.0f : 0.0f);
-                            }
-                            hit = mma32(value_frag(vs, t, n), w, hit);
+                            for (int i = 0; i < 8; ++i)
+                                see[i] = (T)(key0[n] >= 0 && key0[n] + (i >> 2) * 8 + (i & 3) <= p0 ? 1.0f : 0.0f);
+                            hit = mma32(value_frag(lds[1][0], t, n, ln), see, hit);
                         }
 #pragma unroll
                         for (int i = 0; i < 16; ++i)
                             if (hit[i] > 0.0f) o[t][i] += sign ? -kInf : kInf;
                     }
-                }
-            }
-            if (more) {
-                full = whole();
-                odd = put(s0 + NS, buf ^ 1, full);
-                if (full)
                     __syncthreads();
-                else
-                    odd = __syncthreads_or(odd);
+                }
             }
         }
     }
     if (!live) return;
+    // (Addresses are formed anew: kept through the loops they would take registers from them.)
+    const int ln = fresh(lane), out_half = ln >> 5, out_m = P.m0 + wave * 32 + (ln & 31);
+    const int out_tok = (uint32_t)out_m / a.group_div;
+    const int64_t o_head_at = (int64_t)P.h * a.group + (out_m - out_tok * a.group);
     sum = half_sum(sum);
     const float ref = top == -kInf ? 0.0f : top * scale2;
     if (a.splits == 1) {
-        T *dst = (T *)a.out + (int64_t)(P.r.t0 + tok) * a.o_token + head * a.o_head;
+        T *dst = (T *)a.out + (int64_t)(P.r.t0 + out_tok) * a.o_token + o_head_at * a.o_head;
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int i = 0; i < 16; i += 4) {
-                const int d = t * 32 + (i >> 2) * 8 + half * 4;
+                const int d = t * 32 + (i >> 2) * 8 + out_half * 4;
                 if (d >= D) continue;
                 V4 v;
 #pragma unroll
@@ -774,18 +891,18 @@ __global__ __launch_bounds__(THREADS, NK <= 4 && sizeof(T) == 2 ? 2 : 1) void ti
                     for (int e = 0; e < 4; ++e) dst[d + e] = v[e];
                 }
             }
-        if (a.lse && half == 0) a.lse[(int64_t)(P.r.t0 + tok) * (a.heads * a.group) + head] = log_sum(ref, sum);
+        if (a.lse && out_half == 0) a.lse[(int64_t)(P.r.t0 + out_tok) * (a.heads * a.group) + o_head_at] = log_sum(ref, sum);
     } else {
-        const int64_t at = ((int64_t)item * a.splits + split) * a.tile_pairs + wave * 32 + col;
+        const int64_t at = ((int64_t)item * a.splits + split) * a.tile_pairs + wave * 32 + (ln & 31);
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int i = 0; i < 16; i += 4) {
-                const int d = t * 32 + (i >> 2) * 8 + half * 4;
+                const int d = t * 32 + (i >> 2) * 8 + out_half * 4;
                 if (d < D)
                     *reinterpret_cast<f32x4 *>(a.part + at * D + d) = f32x4{o[t][i], o[t][i + 1], o[t][i + 2], o[t][i + 3]};
             }
-        if (half == 0) {
+        if (out_half == 0) {
             a.stat[at * 2] = top == -kInf ? -kInf : top * scale2;
             a.stat[at * 2 + 1] = sum;
         }
@@ -879,7 +996,7 @@ int attention_of(const AttnArgs &a, const Plan &p, hipStream_t stream) {
             rows_kernel<T, 8><<<grid, 256, 0, stream>>>(a);
     } else {
         if (a.dim <= 64)
-            launch_tiles<T, 2, 64>(a, p.waves, grid, stream);
+            launch_tiles<T, 2, sizeof(T) == 4 ? 32 : 64>(a, p.waves, grid, stream);
         else if (a.dim <= 128)
             launch_tiles<T, 4, sizeof(T) == 4 ? 32 : 64>(a, p.waves, grid, stream);
         else
