@@ -78,8 +78,9 @@ struct AttnArgs {
     void *out;
     int64_t o_token, o_head;
     float *lse;
-    float *part, *stat;  // workspace: [item][split][tile_pairs][dim], [item][split][tile_pairs][2]
+    float *part, *stat;  // workspace, items from `whole` on: [item][split][tile_pairs][dim], [item][split][tile_pairs][2]
     int64_t items;       // rows * heads * tiles
+    int64_t whole;       // items [0, whole) are one workgroup each, those behind them `splits`
     int heads, group, dim, keep, tiles, splits, q_aligned, o_aligned;
     int tile_pairs;      // pairs of a tile
     float scale2;        // scale / ln 2
@@ -117,6 +118,31 @@ __device__ __forceinline__ float log_sum(float ref, float sum) {
 // The keys that a tile may read, 16 at a time (slabs: a sixteenth of a page's rows or more lie
 // side by side): the first key of each and its place in the cache, looked up for kSlabs of them at a time.
 constexpr int kSlabs = 256;
+
+// What a workgroup does: share `split` of `splits` of an item. Neighbouring whole items go to one XCD.
+struct Work {
+    uint32_t item;
+    int split, splits;
+};
+
+__device__ __forceinline__ bool find_work(const AttnArgs &a, Work &w) {
+    int64_t idx = grid_index();
+    if (idx < a.whole) {
+        if (a.whole <= kGridX) idx = xcd_linear_id((int)idx, (int)a.whole);
+        w.item = (uint32_t)idx;
+        w.split = 0;
+        w.splits = 1;
+        return true;
+    }
+    idx -= a.whole;
+    if (idx >= (a.items - a.whole) * a.splits) return false;
+    const uint32_t i = (uint32_t)idx / a.split_div;
+    w.item = (uint32_t)a.whole + i;
+    w.split = (int)((uint32_t)idx - i * a.split_div.d);
+    w.splits = a.splits;
+    return true;
+}
+
 struct Slabs {
     int64_t base[kSlabs + 16];  // elements; 0 behind the last
     int key[kSlabs + 16];       // -1: nothing of it is seen
@@ -169,6 +195,14 @@ __device__ __forceinline__ int64_t uniform64(int64_t x) {
 
 __device__ __forceinline__ bool not_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u; }
 
+// Where unit c (16 bytes) of row r of a wave's values lies in its LDS: 32 lanes read two units of eight rows at a
+// time (16-bit types) or four units of two rows, and touch all 64 banks.
+template <int UPR, int SIZE>
+__device__ __forceinline__ int row_unit(int r, int c) {
+    if (SIZE == 4) return c ^ (((r >> 2) & 3) << 2);
+    return UPR >= 16 ? c ^ ((r & 7) << 1) : c ^ (((r >> 1) & 3) << 1);
+}
+
 // One workgroup a (row, head, 16 pairs, share of the row's keys). Its four waves take 32
 // keys in turn, each with a running maximum, sum and output of its own, joined
 // at the end; shares of a row (splits) are joined by join_kernel.
@@ -184,11 +218,9 @@ __global__ __launch_bounds__(256) void rows_kernel(AttnArgs a) {
     __shared__ float w_max[4][16], w_sum[4][16];
     typedef typename VecOf<T, W>::type V;
 
-    const int64_t idx = grid_index();
-    if (idx >= a.items * a.splits) return;
-    const uint32_t item = (uint32_t)idx / a.split_div;
-    const int split = (int)((uint32_t)idx - item * a.split_div.d);
-    const Pairs P = find_pairs(a, item);
+    Work work;
+    if (!find_work(a, work)) return;
+    const Pairs P = find_pairs(a, work.item);
     if (P.r.n == 0) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, part = lane >> 4;
     const int D = a.dim;
@@ -217,8 +249,8 @@ __global__ __launch_bounds__(256) void rows_kernel(AttnArgs a) {
 
     // This share of the row's slabs.
     const int64_t slabs = slabs_of(a, P);
-    const int64_t per = ((slabs + 1) / 2 + a.splits - 1) / a.splits * 2;
-    const int64_t s_lo = min(per * split, slabs), s_hi = min(s_lo + per, slabs);
+    const int64_t per = ((slabs + 1) / 2 + work.splits - 1) / work.splits * 2;
+    const int64_t s_lo = min(per * work.split, slabs), s_hi = min(s_lo + per, slabs);
     const int first_pos = P.r.p0 + (int)((uint32_t)P.m0 / a.group_div);  // position of the tile's first token
 
     constexpr int NT = DP / 16;
@@ -228,64 +260,89 @@ __global__ __launch_bounds__(256) void rows_kernel(AttnArgs a) {
     float top = -kInf, sum = 0.0f;
     T *vt = reinterpret_cast<T *>(lds + wave * kPerWave);
 
+    // Keys go from memory into the operands of the first product, values by rows through LDS, which hands
+    // them out by columns. The next tile's loads start as soon as this one's registers are free.
+    frag_t<T> kf[2][NK];
+    V vf[2][NU];
+    auto fetch_keys = [&](int s) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const T *src = (const T *)a.k_cache + S.base[s + t] + col * D;
+#pragma unroll
+            for (int k = 0; k < NK; ++k) {
+                const int d = k * 32 + part * 8;
+                kf[t][k] = *reinterpret_cast<const frag_t<T> *>(src + (d < D ? d : 0));
+            }
+        }
+    };
+    auto fetch_values = [&](int s) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const T *src = (const T *)a.v_cache + S.base[s + t];
+#pragma unroll
+            for (int i = 0; i < NU; ++i) {
+                const int u = i * 64 + lane, c = u % UPR;
+                vf[t][i] = *reinterpret_cast<const V *>(src + u / UPR * D + (c * W < D ? c * W : 0));
+            }
+        }
+    };
+
     for (int64_t c0 = s_lo; c0 < s_hi; c0 += kSlabs) {
         __syncthreads();
         look_up<256>(S, a, P, c0, s_hi, first_pos);
         __syncthreads();
         const int n_slabs = (int)min(s_hi - c0, (int64_t)kSlabs);
+        if (2 * wave < n_slabs) {
+            fetch_keys(2 * wave);
+            fetch_values(2 * wave);
+        }
         for (int s = 2 * wave; s < n_slabs; s += 8) {
             int key0[2];
-            int64_t base[2];
             bool there[2];
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
                 key0[t] = __builtin_amdgcn_readfirstlane(S.key[s + t]);
-                base[t] = uniform64(S.base[s + t]);
                 there[t] = key0[t] >= 0;
             }
-            if (!there[0] && !there[1]) continue;
-            // Keys: rows of the first product straight from memory.
             f32x4 x[2];
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
                 x[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-                if (there[t]) {
-                    const T *src = (const T *)a.k_cache + base[t] + col * D + part * 8;
 #pragma unroll
-                    for (int k = 0; k < NK; ++k) {
-                        frag_t<T> f = zero_frag<T>();
-                        if (k * 32 + part * 8 < D) f = *reinterpret_cast<const frag_t<T> *>(src + k * 32);
-                        x[t] = mma(f, q[k], x[t]);
-                    }
+                for (int k = 0; k < NK; ++k) {
+                    frag_t<T> f = kf[t][k];
+                    if (k * 32 + part * 8 >= D) f = zero_frag<T>();
+                    x[t] = mma(f, q[k], x[t]);
                 }
             }
-            // Values: to LDS by rows. Rows that no query of the tile sees are zero, whatever
-            // lies there: their weights are zero too, and zero times infinity is not.
-            bool odd = false;  // a value that is not finite
+            if (s + 8 < n_slabs) fetch_keys(s + 8);
+            // Values that no query of the tile sees become zero, whatever lies there: their weights are zero too,
+            // and zero times infinity is not. Of a tile that some see a part of, those that are not finite come
+            // in a pass of their own.
+            bool odd = false;
+            if (!there[0] || !there[1] || max(key0[0], key0[1]) + 15 > first_pos) {
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const bool mixed = there[t] && key0[t] + 15 > first_pos;
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int i = 0; i < NU; ++i) {
+                        const int u = i * 64 + lane;
+                        const bool seen = there[t] && key0[t] + u / UPR <= P.last;
+#pragma unroll
+                        for (int e = 0; e < W; ++e) {
+                            const bool bad = not_finite((float)vf[t][i][e]);
+                            odd = odd || (seen && bad);
+                            if (!seen || bad) vf[t][i][e] = (T)0.0f;
+                        }
+                    }
+            }
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int i = 0; i < NU; ++i) {
-                    const int u = i * 64 + lane, row = u / UPR, c = u % UPR;
-                    V v;
-#pragma unroll
-                    for (int e = 0; e < W; ++e) v[e] = (T)0.0f;
-                    if (there[t] && key0[t] + row <= P.last && c * W < D)
-                        v = *reinterpret_cast<const V *>((const T *)a.v_cache + base[t] + row * D + c * W);
-                    if (mixed) {
-#pragma unroll
-                        for (int e = 0; e < W; ++e)
-                            if (not_finite((float)v[e])) {
-                                odd = true;
-                                v[e] = (T)0.0f;
-                            }
-                    }
-                    const int lr = t * 16 + row;
-                    const int sw = sizeof(T) == 2 ? (lr & (UPR - 1)) : (((lr >> 2) & 3) << 2);
-                    *reinterpret_cast<V *>(vt + lr * DP + (c ^ sw) * W) = v;
+                    const int u = i * 64 + lane, r = t * 16 + u / UPR;
+                    *reinterpret_cast<V *>(vt + r * DP + row_unit<UPR, (int)sizeof(T)>(r, u % UPR) * W) = vf[t][i];
                 }
-            }
+            if (s + 8 < n_slabs) fetch_values(s + 8);
             // Weights.
             float hi8 = -kInf;
 #pragma unroll
@@ -301,14 +358,14 @@ __global__ __launch_bounds__(256) void rows_kernel(AttnArgs a) {
             const float shrink = __builtin_amdgcn_exp2f(top - ref);
             top = next;
             frag_t<T> w;
-            float p[8], total = 0.0f;
+            float total = 0.0f;
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    p[t * 4 + i] = __builtin_amdgcn_exp2f(x[t][i] - ref);
-                    total += p[t * 4 + i];
-                    w[t * 4 + i] = (T)p[t * 4 + i];
+                    const float p = __builtin_amdgcn_exp2f(x[t][i] - ref);
+                    total += p;
+                    w[t * 4 + i] = (T)p;
                 }
             sum = sum * shrink + total;
             if (__ballot(shrink != 1.0f)) {
@@ -331,7 +388,7 @@ __global__ __launch_bounds__(256) void rows_kernel(AttnArgs a) {
                     for (int b = 0; b < 2; ++b) {
                         const int lr = b * 16 + part * 4 + (col >> 2);
                         const int c = t * 2 + ((col & 3) >> 1);
-                        T *src = vt + lr * DP + ((c ^ (lr & (UPR - 1))) * W) + (col & 1) * 4;
+                        T *src = vt + lr * DP + row_unit<UPR, 2>(lr, c) * W + (col & 1) * 4;
                         u.h[b] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)src);
                     }
                     f = u.f;
@@ -339,7 +396,7 @@ __global__ __launch_bounds__(256) void rows_kernel(AttnArgs a) {
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         const int lr = (i >> 2) * 16 + part * 4 + (i & 3), d = t * 16 + col;
-                        f[i] = vt[lr * DP + (((d >> 2) ^ (((lr >> 2) & 3) << 2)) << 2) + (d & 3)];
+                        f[i] = vt[lr * DP + row_unit<UPR, 4>(lr, d >> 2) * 4 + (d & 3)];
                     }
                 }
                 o[t] = mma(f, w, o[t]);
@@ -350,11 +407,8 @@ __global__ __launch_bounds__(256) void rows_kernel(AttnArgs a) {
                 for (int t = 0; t < 2; ++t) {
                     if (!there[t] || key0[t] + 15 <= first_pos) continue;
                     for (int kr = 0; kr < 16; ++kr) {
-                        const float p0 = p[t * 4], p1 = p[t * 4 + 1], p2 = p[t * 4 + 2], p3 = p[t * 4 + 3];
-                        const float mine = (kr & 3) == 0 ? p0 : (kr & 3) == 1 ? p1 : (kr & 3) == 2 ? p2 : p3;
-                        const float weight = __shfl(mine, (kr >> 2) * 16 + col);
                         if (key0[t] + kr > pos) continue;
-                        const T *src = (const T *)a.v_cache + base[t] + kr * D;
+                        const T *src = (const T *)a.v_cache + S.base[s + t] + kr * D;
 #pragma unroll
                         for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -362,7 +416,7 @@ __global__ __launch_bounds__(256) void rows_kernel(AttnArgs a) {
                                 const int d = n * 16 + part * 4 + i;
                                 if (d >= D) continue;
                                 const float v = (float)src[d];
-                                if (not_finite(v)) o[n][i] += weight * v;
+                                if (not_finite(v)) o[n][i] += v;
                             }
                     }
                 }
@@ -397,12 +451,12 @@ __global__ __launch_bounds__(256) void rows_kernel(AttnArgs a) {
             l += f * w_sum[w][c];
             acc += f * reinterpret_cast<const float *>(lds + w * kPerWave)[c * (DP + 4) + d];
         }
-        if (a.splits == 1) {
+        if (work.splits == 1) {
             const int mm = P.m0 + c, tk = (uint32_t)mm / a.group_div, g = P.h * a.group + (mm - tk * a.group);
             ((T *)a.out)[(int64_t)(P.r.t0 + tk) * a.o_token + (int64_t)g * a.o_head + d] = (T)weighted(acc, l);
             if (a.lse && d == 0) a.lse[(int64_t)(P.r.t0 + tk) * (a.heads * a.group) + g] = log_sum(ref, l);
         } else {
-            const int64_t at = ((int64_t)item * a.splits + split) * 16 + c;
+            const int64_t at = ((work.item - a.whole) * a.splits + work.split) * 16 + c;
             a.part[at * D + d] = acc;
             if (d == 0) {
                 a.stat[at * 2] = mx;
@@ -486,13 +540,9 @@ __global__ __launch_bounds__(THREADS, NK <= 4 && sizeof(T) == 2 ? 2 : 1) void ti
     typedef typename VecOf<T, W>::type V;
     typedef typename VecOf<T, 4>::type V4;
 
-    int64_t idx = grid_index();
-    const int64_t all = a.items * a.splits;
-    if (idx >= all) return;
-    if (gridDim.y == 1) idx = xcd_linear_id((int)idx, (int)all);
-    const uint32_t item = (uint32_t)idx / a.split_div;
-    const int split = (int)((uint32_t)idx - item * a.split_div.d);
-    const Pairs P = find_pairs(a, item);
+    Work work;
+    if (!find_work(a, work)) return;
+    const Pairs P = find_pairs(a, work.item);
     if (P.r.n == 0) return;
     const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -526,8 +576,8 @@ __global__ __launch_bounds__(THREADS, NK <= 4 && sizeof(T) == 2 ? 2 : 1) void ti
     const bool busy = P.m0 + wave * 32 < P.end;
 
     const int64_t slabs = slabs_of(a, P);
-    const int64_t per = ((slabs + NS - 1) / NS + a.splits - 1) / a.splits * NS;
-    const int64_t s_lo = min(per * split, slabs), s_hi = min(s_lo + per, slabs);
+    const int64_t per = ((slabs + NS - 1) / NS + work.splits - 1) / work.splits * NS;
+    const int64_t s_lo = min(per * work.split, slabs), s_hi = min(s_lo + per, slabs);
 
     f32x16 o[NT];
 #pragma unroll
@@ -873,7 +923,7 @@ __global__ __launch_bounds__(THREADS, NK <= 4 && sizeof(T) == 2 ? 2 : 1) void ti
     const int64_t o_head_at = (int64_t)P.h * a.group + (out_m - out_tok * a.group);
     sum = half_sum(sum);
     const float ref = top == -kInf ? 0.0f : top * scale2;
-    if (a.splits == 1) {
+    if (work.splits == 1) {
         T *dst = (T *)a.out + (int64_t)(P.r.t0 + out_tok) * a.o_token + o_head_at * a.o_head;
 #pragma unroll
         for (int t = 0; t < NT; ++t)
@@ -893,7 +943,7 @@ __global__ __launch_bounds__(THREADS, NK <= 4 && sizeof(T) == 2 ? 2 : 1) void ti
             }
         if (a.lse && out_half == 0) a.lse[(int64_t)(P.r.t0 + out_tok) * (a.heads * a.group) + o_head_at] = log_sum(ref, sum);
     } else {
-        const int64_t at = ((int64_t)item * a.splits + split) * a.tile_pairs + wave * 32 + (ln & 31);
+        const int64_t at = ((work.item - a.whole) * a.splits + work.split) * a.tile_pairs + wave * 32 + (ln & 31);
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -909,38 +959,71 @@ __global__ __launch_bounds__(THREADS, NK <= 4 && sizeof(T) == 2 ? 2 : 1) void ti
     }
 }
 
-// Joins the shares of a pair: one workgroup a (row, head, tile, pair).
+// Joins the shares of a pair: one workgroup a (row, head, tile, pair). The factors of the shares are formed by a
+// thread each, then the shares are summed by 256 / (dim / 4) groups of threads, four components a thread, eight loads ahead.
 template <typename T>
 __global__ __launch_bounds__(256) void join_kernel(AttnArgs a) {
+    __shared__ float factor[512];
+    __shared__ float red[8];
+    __shared__ f32x4 sums[256];
     const int64_t idx = grid_index();
-    if (idx >= a.items * a.tile_pairs) return;
-    const uint32_t item = (uint32_t)idx / a.pair_div;
+    if (idx >= (a.items - a.whole) * a.tile_pairs) return;
+    const uint32_t item = (uint32_t)idx / a.pair_div;  // from `whole` on
     const int c = (int)((uint32_t)idx - item * a.pair_div.d);
-    const Pairs P = find_pairs(a, item);
+    const Pairs P = find_pairs(a, (uint32_t)a.whole + item);
     if (P.r.n == 0 || P.m0 + c >= P.end) return;
     const int step = a.tile_pairs;  // from share to share
     const float *stat = a.stat + ((int64_t)item * a.splits * step + c) * 2;
     const float *part = a.part + ((int64_t)item * a.splits * step + c) * a.dim;
-    float mx = -kInf;
-    for (int s = 0; s < a.splits; ++s) mx = fmaxf(mx, stat[s * step * 2]);
-    const int m = P.m0 + c, tok = (uint32_t)m / a.group_div, g = P.h * a.group + (m - tok * a.group);
-    const int d = threadIdx.x;
-    if (d >= a.dim) return;
-    const float ref = mx == -kInf ? 0.0f : mx;
-    float acc = 0.0f, l = 0.0f;
-    for (int s = 0; s < a.splits; ++s) {
-        const float x = stat[s * step * 2], y = stat[s * step * 2 + 1];
-        if (x == -kInf && y == 0.0f) continue;
-        const float f = __builtin_amdgcn_exp2f(x - ref);
-        l += f * y;
-        acc += f * part[(int64_t)s * step * a.dim + d];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    float x[2], y[2], mx = -kInf;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int s = tid + i * 256;
+        x[i] = s < a.splits ? stat[s * step * 2] : -kInf;
+        y[i] = s < a.splits ? stat[s * step * 2 + 1] : 0.0f;
+        mx = fmaxf(mx, x[i]);
     }
-    ((T *)a.out)[(int64_t)(P.r.t0 + tok) * a.o_token + (int64_t)g * a.o_head + d] = (T)weighted(acc, l);
-    if (a.lse && d == 0) a.lse[(int64_t)(P.r.t0 + tok) * (a.heads * a.group) + g] = log_sum(ref, l);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
+    if (lane == 0) red[wave] = mx;
+    __syncthreads();
+    mx = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    const float ref = mx == -kInf ? 0.0f : mx;
+    float l = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const float f = __builtin_amdgcn_exp2f(x[i] - ref);
+        factor[tid + i * 256] = f;
+        l += f * y[i];
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) l += __shfl_xor(l, o);
+    if (lane == 0) red[4 + wave] = l;
+    __syncthreads();
+    l = (red[4] + red[5]) + (red[6] + red[7]);
+
+    const int quads = a.dim / 4, groups = 256 / quads, g = tid / quads, u = tid - g * quads;
+    f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (g < groups) {
+        const int64_t stride = (int64_t)step * a.dim;
+#pragma unroll 8
+        for (int s = g; s < a.splits; s += groups)
+            acc += factor[s] * *reinterpret_cast<const f32x4 *>(part + s * stride + u * 4);
+    }
+    sums[tid] = acc;
+    __syncthreads();
+    if (tid >= quads) return;
+    for (int k = 1; k < groups; ++k) acc += sums[k * quads + u];
+    const int m = P.m0 + c, tok = (uint32_t)m / a.group_div, head = P.h * a.group + (m - tok * a.group);
+    T *dst = (T *)a.out + (int64_t)(P.r.t0 + tok) * a.o_token + (int64_t)head * a.o_head + u * 4;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) dst[e] = (T)weighted(acc[e], l);
+    if (a.lse && tid == 0) a.lse[(int64_t)(P.r.t0 + tok) * (a.heads * a.group) + head] = log_sum(ref, l);
 }
 
 struct Plan {
-    int64_t items;
+    int64_t items, whole;
     int waves;  // of the tiles kernel; 0: the rows kernel
     int tile_pairs, tiles, splits;
     int64_t part_bytes, bytes;
@@ -961,15 +1044,19 @@ bool plan_of(int dtype, const spconv_batch *B, int q_heads, int heads, int dim, 
     p->tiles = (int)((pairs + p->tile_pairs - 1) / p->tile_pairs);
     p->items = rows_of(B) * heads * p->tiles;
     if (p->items >= ((int64_t)1 << 27)) return false;
-    // Shares of a row's keys: enough workgroups for two on every CU, 256 keys each at least.
+    // The GPU holds `slots` workgroups at a time: one of eight waves on a CU, two of the smaller ones. Items that do not
+    // fill a round of them are split along their keys (128 keys a share at least), so that they do.
+    const int64_t slots = p->waves == 8 ? 256 : 512;
     const int64_t keys = (int64_t)(keep ? keep : B->max_blocks) * B->block;
-    int64_t splits = (512 + p->items - 1) / p->items;
-    splits = std::min<int64_t>(splits, (keys + 255) / 256);
+    const int64_t rest = p->items % slots;
+    // (Behind sixteen full rounds the last one does not matter.)
+    const int64_t splits = rest && p->items <= 16 * slots ? std::min(slots / rest, (keys + 127) / 128) : 1;
     p->splits = (int)std::max<int64_t>(1, splits);
+    p->whole = p->splits > 1 ? p->items - rest : p->items;
     p->part_bytes = p->bytes = 0;
     if (p->splits > 1) {
-        p->part_bytes = p->items * p->splits * p->tile_pairs * dim * 4;
-        p->bytes = p->part_bytes + p->items * p->splits * p->tile_pairs * 2 * 4;
+        p->part_bytes = rest * p->splits * p->tile_pairs * dim * 4;
+        p->bytes = p->part_bytes + rest * p->splits * p->tile_pairs * 2 * 4;
     }
     return true;
 }
@@ -986,7 +1073,7 @@ void launch_tiles(const AttnArgs &a, int waves, dim3 grid, hipStream_t stream) {
 
 template <typename T>
 int attention_of(const AttnArgs &a, const Plan &p, hipStream_t stream) {
-    const dim3 grid = grid_of(a.items * a.splits);
+    const dim3 grid = grid_of(a.whole + (a.items - a.whole) * a.splits);
     if (p.waves == 0) {
         if (a.dim <= 64)
             rows_kernel<T, 2><<<grid, 256, 0, stream>>>(a);
@@ -1004,7 +1091,7 @@ int attention_of(const AttnArgs &a, const Plan &p, hipStream_t stream) {
     }
     if (hipGetLastError() != hipSuccess) return SPCONV_EHIP;
     if (a.splits > 1) {
-        join_kernel<T><<<grid_of(a.items * a.tile_pairs), 256, 0, stream>>>(a);
+        join_kernel<T><<<grid_of((a.items - a.whole) * a.tile_pairs), 256, 0, stream>>>(a);
         return launched();
     }
     return SPCONV_OK;
@@ -1036,7 +1123,7 @@ extern "C" int spconv_block_attention(int dtype, const spconv_batch *batch, cons
         return SPCONV_EINVAL;
     if (p.bytes > 0 && (workspace == nullptr || !aligned16(workspace) || workspace_bytes < p.bytes)) return SPCONV_EINVAL;
     AttnArgs a{*batch, q, q_token, q_head, k_cache, v_cache, blocks, counts, out, out_token, out_head, lse,
-               (float *)workspace, nullptr, p.items, heads, q_heads / heads, dim, keep, p.tiles, p.splits,
+               (float *)workspace, nullptr, p.items, p.whole, heads, q_heads / heads, dim, keep, p.tiles, p.splits,
                rows_aligned16(q, q_token, q_head, size_of(dtype)),
                rows_aligned16(out, out_token, out_head, size_of(dtype)), p.tile_pairs, scale * kLog2e,
                make_div((uint32_t)p.tiles), make_div((uint32_t)heads), make_div((uint32_t)(q_heads / heads)),
