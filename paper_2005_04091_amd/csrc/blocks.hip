@@ -1,5 +1,6 @@
 // Block scores and block selection (spconv_block_scores, spconv_select_blocks).
 #include "batch.h"
+#include "split.h"
 
 namespace {
 
@@ -15,7 +16,7 @@ struct ScoreArgs {
     const float *sums;
     float *scores;
     int64_t items;
-    int heads, group, dim, tiles;  // tiles: workgroups of 64 blocks along the table
+    int heads, group, dim, tiles;  // tiles: workgroups of 256 blocks along the table
     Div tile_div, head_div, group_div;
     int aligned;
 };
@@ -39,80 +40,214 @@ __device__ __forceinline__ Floats<8> load_query(const T *p, bool aligned) {
     return r;
 }
 
-// One wave 16 blocks of a (row, head): their key sums stay in registers as the
-// rows of 16x16 fp32 matrix tiles, and the row's (token, head) pairs pass as columns, 16 a
-// tile. Lane l holds components 8*(l/16) .. +8 of every 32 of block l%16, and of pair
-// l%16: the order of the components in a product is free, so each instruction
-// takes one of the eight from every lane.
-template <typename T, int NK>
+// bf16 parts of queries: bf16 ones are one part, fp16 ones (11 bits) two, fp32 ones three; exact but for fp32's
+// least bits below 2^-110.
+template <typename T>
+constexpr int kParts = sizeof(T) == 4 ? 3 : 2;
+template <>
+constexpr int kParts<__bf16> = 1;
+
+// Parts of eight components, one 16-byte vector each.
+template <typename T>
+__device__ __forceinline__ void query_parts(const Floats<8> &x, u32x4_t (&p)[kParts<T>]) {
+    Parts s;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) split2(s, i, x.v[2 * i], x.v[2 * i + 1]);
+    p[0] = s.h;
+    if constexpr (kParts<T> > 1) p[1] = s.m;
+    if constexpr (kParts<T> > 2) p[2] = s.l;
+}
+
+__device__ __forceinline__ f32x4 mma_bits(u32x4_t a, u32x4_t b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
+}
+
+// Unit (16 bytes) u of pair m's row of one part in LDS: 16 lanes read one unit of 16 rows.
+template <int UPR>
+__device__ __forceinline__ int pair_unit(int m, int u) {
+    return UPR >= 16 ? u ^ (m & 15) : u ^ ((m >> 1) & (UPR - 1));
+}
+
+// One workgroup 256 blocks of a (row, head), a wave 16 at a time: their key sums, as three bf16 parts of each
+// fp32 value (split.h), are the rows of 16x16 matrix tiles, and the row's (token, head) pairs pass
+// as columns. A product takes the part products of weight 2^-16 or more (three for bf16 queries, five for
+// fp16, six for fp32), which is closer than a chain of fp32 products, at a fifth to a tenth of the time of the fp32
+// matrix instructions. Lane l holds components 8*(l/16) .. +8 of every 32 of block l%16, and of pair l%16.
+// Pairs: 16 or less (ONE) stay in registers; more lie in LDS, kPairs at a time. Sums that are not
+// finite, or whose products are not, are taken again in fp32.
+// Bound by the sums' bytes for single tokens, by the matrix unit for prompts.
+template <typename T, int NK, bool ONE>
 __global__ __launch_bounds__(256) void scores_kernel(ScoreArgs a) {
+    constexpr int DP = NK * 32, UPR = DP / 8, NP = kParts<T>, kPairs = ONE ? 16 : (DP == 256 || NP == 3) ? 64 : 128;
+    __shared__ __attribute__((aligned(16))) uint16_t qs[ONE ? 1 : kPairs * NP * DP];
+    __shared__ float kept[256];  // maxima of the chunks of pairs so far
     const int64_t idx = grid_index();
     if (idx >= a.items) return;
     const uint32_t rh = (uint32_t)idx / a.tile_div;
     const int tile = (int)((uint32_t)idx - rh * a.tile_div.d);
     const int row = (int)(rh / a.head_div), h = (int)(rh - row * a.head_div.d);
     const spconv_batch &B = a.B;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int c0 = tile * 64 + wave * 16;
-    if (c0 >= B.max_blocks) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, part = lane >> 4;
     const Row r = find_row(B, row);
     const int p1 = r.n > 0 ? r.p0 + r.n - 1 : -1;
     const int visible = p1 < 0 ? 0 : min(p1 / B.block + 1, B.max_blocks);
+    const int c_base = tile * 256;
     float *out = a.scores + ((int64_t)row * a.heads + h) * B.max_blocks;
-    if (c0 >= visible) {
-        if (lane < 16 && c0 + lane < B.max_blocks) out[c0 + lane] = -kInf;
+    if (c_base >= visible) {
+        const int j = c_base + (int)threadIdx.x;
+        if (j < B.max_blocks) out[j] = -kInf;
         return;
     }
-    // Key sums.
-    const int col = lane & 15, part = lane >> 4;
-    Floats<8> s[NK];
-    const int page = c0 + col < visible ? page_of(B, r.b, c0 + col) : -1;
-#pragma unroll
-    for (int k = 0; k < NK; ++k) {
-        const int d = k * 32 + part * 8;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) s[k].v[i] = 0.0f;
-        if (page >= 0 && d < a.dim) s[k] = load_query(a.sums + ((int64_t)page * a.heads + h) * a.dim + d, true);
-    }
-    // Rows of the result are blocks c0 + 4*part + i, columns pairs.
-    float best[4], inv[4];
-    int key0[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        best[i] = -kInf;
-        const int j = c0 + part * 4 + i;
-        const bool there = __shfl(page, part * 4 + i) >= 0;
-        key0[i] = there ? j * B.block : 0x7fffffff;
-        inv[i] = 1.0f / (float)clamp_int(r.kv - j * B.block, 1, B.block);
-    }
+    // Pages of this wave's blocks: tile i of it is blocks c_base + (4*i + wave)*16 and on.
+    const int mine = c_base + ((lane >> 4) * 4 + wave) * 16 + col;
+    const int pages = mine < visible ? page_of(B, r.b, mine) : -1;
     const int pairs = r.n * a.group;
-    for (int m0 = 0; m0 < pairs; m0 += 16) {
-        const int m = m0 + col;
+    auto query_at = [&](int m) {
         const int i = (uint32_t)m / a.group_div, g = m - i * (int)a.group_div.d;
-        const int p = m < pairs ? r.p0 + i : -1;
-        const T *q = (const T *)a.q + (int64_t)(r.t0 + i) * a.q_token + (int64_t)(h * a.group + g) * a.q_head;
-        f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+        return (const T *)a.q + (int64_t)(r.t0 + i) * a.q_token + (int64_t)(h * a.group + g) * a.q_head;
+    };
+    Floats<8> none;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) none.v[i] = 0.0f;
+
+    u32x4_t q1[ONE ? NK : 1][NP];
+    if constexpr (ONE) {
 #pragma unroll
         for (int k = 0; k < NK; ++k) {
             const int d = k * 32 + part * 8;
-            Floats<8> x;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x.v[e] = 0.0f;
-            if (p >= 0 && d < a.dim) x = load_query(q + d, a.aligned);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(s[k].v[e], x.v[e], acc, 0, 0, 0);
+            query_parts<T>(col < pairs && d < a.dim ? load_query(query_at(col) + d, a.aligned) : none, q1[k]);
         }
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (p >= key0[e]) best[e] = fmaxf(best[e], acc[e] * inv[e]);
     }
+    // Key sums of tile i, fp32.
+    Floats<8> raw[NK];
+    auto fetch = [&](int i) {
+        const int page = __shfl(pages, i * 16 + col);
 #pragma unroll
-    for (int o = 8; o > 0; o >>= 1)
+        for (int k = 0; k < NK; ++k) {
+            const int d = k * 32 + part * 8;
+            raw[k] = page >= 0 && d < a.dim ? load_query(a.sums + ((int64_t)page * a.heads + h) * a.dim + d, true) : none;
+        }
+    };
+    // Rows of a result are blocks c0 + 4*part + e, columns pairs.
+    auto bounds = [&](int i, int (&key0)[4], float (&inv)[4]) {
+        const int c0 = c_base + (i * 4 + wave) * 16;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) best[e] = fmaxf(best[e], __shfl_xor(best[e], o));
-    const int j = c0 + part * 4 + (col & 3);
-    const float v = col == 0 ? best[0] : col == 1 ? best[1] : col == 2 ? best[2] : best[3];
-    if (col < 4 && j < B.max_blocks) out[j] = v;
+        for (int e = 0; e < 4; ++e) {
+            const int j = c0 + part * 4 + e;
+            key0[e] = __shfl(pages, i * 16 + part * 4 + e) >= 0 ? j * B.block : 0x7fffffff;
+            inv[e] = 1.0f / (float)clamp_int(r.kv - j * B.block, 1, B.block);
+        }
+    };
+    // Maxima over the columns, to lane 16*part + e of each four rows.
+    auto finish = [&](int i, float (&best)[4]) {
+#pragma unroll
+        for (int o = 8; o > 0; o >>= 1)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) best[e] = fmaxf(best[e], __shfl_xor(best[e], o));
+        const int at = (i * 4 + wave) * 16 + part * 4 + (col & 3), j = c_base + at;
+        const float v = (col & 3) == 0 ? best[0] : (col & 3) == 1 ? best[1] : (col & 3) == 2 ? best[2] : best[3];
+        if (col < 4) kept[at] = v;
+        if (col < 4 && j < B.max_blocks) out[j] = v;
+    };
+
+    const int last = (visible - c_base - wave * 16 + 63) >> 6;  // tiles of this wave that have visible blocks (0 or less: none)
+    const int tiles = min(max(last, 0), 4);
+    uint32_t again = 0;
+    for (int m_base = 0; m_base < pairs; m_base += kPairs) {
+        const int n_pairs = min(pairs - m_base, kPairs);
+        if (tiles > 0) fetch(0);
+        if constexpr (!ONE) {
+            __syncthreads();
+            for (int u = threadIdx.x; u < n_pairs * UPR; u += 256) {
+                const int m = u / UPR, d = (u % UPR) * 8;
+                u32x4_t p[NP];
+                query_parts<T>(d < a.dim ? load_query(query_at(m_base + m) + d, a.aligned) : none, p);
+#pragma unroll
+                for (int i = 0; i < NP; ++i)
+                    *reinterpret_cast<u32x4_t *>(qs + ((m * NP + i) * UPR + pair_unit<UPR>(m, u % UPR)) * 8) = p[i];
+            }
+            __syncthreads();
+        }
+        for (int i = 0; i < tiles; ++i) {
+            Parts s[NK];
+#pragma unroll
+            for (int k = 0; k < NK; ++k)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) split2(s[k], e, raw[k].v[2 * e], raw[k].v[2 * e + 1]);
+            if (i + 1 < tiles) fetch(i + 1);
+            int key0[4];
+            float inv[4], best[4];
+            bounds(i, key0, inv);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) best[e] = m_base > 0 ? kept[(i * 4 + wave) * 16 + part * 4 + e] : -kInf;
+            bool bad = false;
+            for (int m0 = 0; m0 < n_pairs; m0 += 16) {
+                const int m = m0 + col;
+                const int p = m < n_pairs ? r.p0 + (int)((uint32_t)(m_base + m) / a.group_div) : -1;
+                f32x4 hi = {0.0f, 0.0f, 0.0f, 0.0f}, lo = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int k = 0; k < NK; ++k) {
+                    u32x4_t x[NP];
+                    if constexpr (ONE) {
+#pragma unroll
+                        for (int e = 0; e < NP; ++e) x[e] = q1[k][e];
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < NP; ++e)
+                            x[e] = *reinterpret_cast<const u32x4_t *>(qs + ((m * NP + e) * UPR + pair_unit<UPR>(m, k * 4 + part)) * 8);
+                    }
+                    hi = mma_bits(s[k].h, x[0], hi);
+                    lo = mma_bits(s[k].m, x[0], lo);
+                    lo = mma_bits(s[k].l, x[0], lo);
+                    if constexpr (NP > 1) {
+                        lo = mma_bits(s[k].h, x[1], lo);
+                        lo = mma_bits(s[k].m, x[1], lo);
+                    }
+                    if constexpr (NP > 2) lo = mma_bits(s[k].h, x[2], lo);
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float v = (hi[e] + lo[e]) * inv[e];
+                    if (p >= key0[e]) {
+                        bad = bad || !(fabsf(v) < kInf);
+                        best[e] = fmaxf(best[e], v);
+                    }
+                }
+            }
+            if (__ballot(bad)) again |= 1u << i;
+            finish(i, best);
+        }
+        // Tiles of this wave behind the visible blocks.
+        if (m_base == 0)
+            for (int i = tiles; i < 4; ++i) {
+                const int j = c_base + (i * 4 + wave) * 16 + lane;
+                if (lane < 16 && j < B.max_blocks) out[j] = -kInf;
+            }
+    }
+    // Again in fp32.
+    for (int i = 0; again != 0; ++i, again >>= 1) {
+        if (!(again & 1)) continue;
+        fetch(i);
+        int key0[4];
+        float inv[4], best[4] = {-kInf, -kInf, -kInf, -kInf};
+        bounds(i, key0, inv);
+        for (int m0 = 0; m0 < pairs; m0 += 16) {
+            const int m = m0 + col;
+            const int p = m < pairs ? r.p0 + (int)((uint32_t)m / a.group_div) : -1;
+            f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int k = 0; k < NK; ++k) {
+                const int d = k * 32 + part * 8;
+                const Floats<8> x = p >= 0 && d < a.dim ? load_query(query_at(m) + d, a.aligned) : none;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(raw[k].v[e], x.v[e], acc, 0, 0, 0);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (p >= key0[e]) best[e] = fmaxf(best[e], acc[e] * inv[e]);
+        }
+        finish(i, best);
+    }
 }
 
 struct SelectArgs {
@@ -305,16 +440,21 @@ __global__ __launch_bounds__(1024) void select_block_kernel(SelectArgs a, int pe
     for (int i = mine + (int)threadIdx.x; i < a.keep; i += 1024) blocks[i] = -1;
 }
 
-template <typename T>
-int scores_of(ScoreArgs &a, hipStream_t stream) {
+template <typename T, bool ONE>
+int scores_of(const ScoreArgs &a, hipStream_t stream) {
     const dim3 grid = grid_of(a.items);
     if (a.dim <= 64)
-        scores_kernel<T, 2><<<grid, 256, 0, stream>>>(a);
+        scores_kernel<T, 2, ONE><<<grid, 256, 0, stream>>>(a);
     else if (a.dim <= 128)
-        scores_kernel<T, 4><<<grid, 256, 0, stream>>>(a);
+        scores_kernel<T, 4, ONE><<<grid, 256, 0, stream>>>(a);
     else
-        scores_kernel<T, 8><<<grid, 256, 0, stream>>>(a);
+        scores_kernel<T, 8, ONE><<<grid, 256, 0, stream>>>(a);
     return launched();
+}
+
+template <typename T>
+int scores_by_pairs(const ScoreArgs &a, hipStream_t stream) {
+    return a.B.q_block * a.group <= 16 ? scores_of<T, true>(a, stream) : scores_of<T, false>(a, stream);
 }
 
 }  // namespace
@@ -325,15 +465,15 @@ extern "C" int spconv_block_scores(int dtype, const spconv_batch *batch, const v
     if (!batch_ok(batch) || !batch_arrays_ok(batch) || !dtype_ok(dtype) || q == nullptr || sums == nullptr ||
         scores == nullptr || !heads_ok(q_heads, heads, dim) || q_token < 0 || q_head < 0 || !aligned16(sums))
         return SPCONV_EINVAL;
-    const int tiles = (batch->max_blocks + 63) / 64;
+    const int tiles = (batch->max_blocks + 255) / 256;
     const int64_t rows = rows_of(batch);
     if (rows * heads * tiles >= ((int64_t)1 << 31)) return SPCONV_EINVAL;
     ScoreArgs a{*batch, q, q_token, q_head, sums, scores, rows * heads * tiles, heads, q_heads / heads, dim, tiles,
                 make_div((uint32_t)tiles), make_div((uint32_t)heads), make_div((uint32_t)(q_heads / heads)),
                 rows_aligned16(q, q_token, q_head, size_of(dtype))};
-    if (dtype == SPCONV_F32) return scores_of<float>(a, stream);
-    if (dtype == SPCONV_F16) return scores_of<_Float16>(a, stream);
-    return scores_of<__bf16>(a, stream);
+    if (dtype == SPCONV_F32) return scores_by_pairs<float>(a, stream);
+    if (dtype == SPCONV_F16) return scores_by_pairs<_Float16>(a, stream);
+    return scores_by_pairs<__bf16>(a, stream);
 }
 
 extern "C" int spconv_select_blocks(const spconv_batch *batch, int heads, const float *scores, int keep, int sink,
