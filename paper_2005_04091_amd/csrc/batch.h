@@ -89,8 +89,8 @@ inline dim3 grid_of(int64_t n) {
 
 __device__ __forceinline__ int64_t grid_index() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
 
-// The last sequence b whose start, q_start[b]/div + mul*b, is at most x, found by the
-// whole wave (64 sequences a step), and its tokens. The starts do not decrease; where
+// The last sequence b whose start, q_start[b]/div + mul*b, is at most x (the same for the whole wave, as is
+// the result), found by the whole wave, 64 sequences a step, and its tokens. The starts do not decrease; where
 // they do (the array is the caller's) some sequence or none comes out, with
 // its tokens taken into the batch.
 struct Seq {
@@ -102,9 +102,12 @@ struct Seq {
 
 __device__ __forceinline__ int clamp_int(int x, int lo, int hi) { return min(max(x, lo), hi); }
 
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
 __device__ __forceinline__ Seq find_seq(const spconv_batch &B, int x, int div, int mul) {
     Seq s;
     const int tokens = (int)B.tokens;
+    x = uniform(x);
     if (B.q_start == nullptr) {
         s.b = x;
         s.first = x;
@@ -125,11 +128,11 @@ __device__ __forceinline__ Seq find_seq(const spconv_batch &B, int x, int div, i
         s.b = count - 1;
         s.first = s.n = s.at = s.kv = 0;
         if (s.b < 0) return s;
-        s.first = clamp_int(B.q_start[s.b], 0, tokens);
-        s.n = max(clamp_int(B.q_start[s.b + 1], 0, tokens) - s.first, 0);
+        s.first = clamp_int(uniform(B.q_start[s.b]), 0, tokens);
+        s.n = max(clamp_int(uniform(B.q_start[s.b + 1]), 0, tokens) - s.first, 0);
         s.at = (int)((int64_t)x - (s.first / div) - (int64_t)mul * s.b);
     }
-    s.kv = clamp_int(B.kv_len[s.b], 0, B.max_blocks * B.block);
+    s.kv = clamp_int(uniform(B.kv_len[s.b]), 0, B.max_blocks * B.block);
     return s;
 }
 

@@ -16,26 +16,33 @@ struct ScoreArgs {
     const float *sums;
     float *scores;
     int64_t items;
-    int heads, group, dim, tiles;  // tiles: workgroups of 256 blocks along the table
+    int heads, group, dim, tiles;  // tiles: workgroups along the table
     Div tile_div, head_div, group_div;
     int aligned;
 };
 
-// Eight components of a query from d on (dim is a multiple of 8: all there or none).
+// The eight components of a row that lane part `part` holds of every 32 from d0 on: d0 + 4*part .. +4 and 16 behind
+// them (the order of the components in a product is free; so the four parts' 16-byte loads of fp32 rows are neighbours).
+// dim is a multiple of 8: each half is all there or not.
 template <typename T>
-__device__ __forceinline__ Floats<8> load_query(const T *p, bool aligned) {
+__device__ __forceinline__ Floats<8> load_part(const T *p, int d0, int part, int dim, bool aligned) {
     Floats<8> r;
-    if (aligned) {
-        constexpr int W = kPer16<T>;
 #pragma unroll
-        for (int i = 0; i < 8; i += W) {
-            const Floats<W> f = load_floats<T, W>(p + i);
+    for (int i = 0; i < 2; ++i) {
+        const int d = d0 + i * 16 + part * 4;
+        Floats<4> f;
 #pragma unroll
-            for (int k = 0; k < W; ++k) r.v[i + k] = f.v[k];
+        for (int k = 0; k < 4; ++k) f.v[k] = 0.0f;
+        if (d < dim) {
+            if (aligned) {
+                f = load_floats<T, 4>(p + d);
+            } else {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) f.v[k] = (float)p[d + k];
+            }
         }
-    } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) r.v[i] = (float)p[i];
+        for (int k = 0; k < 4; ++k) r.v[i * 4 + k] = f.v[k];
     }
     return r;
 }
@@ -68,19 +75,27 @@ __device__ __forceinline__ int pair_unit(int m, int u) {
     return UPR >= 16 ? u ^ (m & 15) : u ^ ((m >> 1) & (UPR - 1));
 }
 
-// One workgroup 256 blocks of a (row, head), a wave 16 at a time: their key sums, as three bf16 parts of each
+// Blocks of a workgroup: with one tile of pairs a wave has 16, and more waves hide the loads; with many, 32.
+constexpr int score_blocks(bool one) { return one ? 64 : 256; }
+
+// One workgroup 64 or 256 blocks of a (row, head), a wave 16 at a time: their key sums, as three bf16 parts of each
 // fp32 value (split.h), are the rows of 16x16 matrix tiles, and the row's (token, head) pairs pass
 // as columns. A product takes the part products of weight 2^-16 or more (three for bf16 queries, five for
 // fp16, six for fp32), which is closer than a chain of fp32 products, at a fifth to a tenth of the time of the fp32
-// matrix instructions. Lane l holds components 8*(l/16) .. +8 of every 32 of block l%16, and of pair l%16.
+// matrix instructions. Lane l holds eight components of every 32 of block l%16, and of pair l%16.
 // Pairs: 16 or less (ONE) stay in registers; more lie in LDS, kPairs at a time. Sums that are not
 // finite, or whose products are not, are taken again in fp32.
 // Bound by the sums' bytes for single tokens, by the matrix unit for prompts.
 template <typename T, int NK, bool ONE>
-__global__ __launch_bounds__(256) void scores_kernel(ScoreArgs a) {
-    constexpr int DP = NK * 32, UPR = DP / 8, NP = kParts<T>, kPairs = ONE ? 16 : (DP == 256 || NP == 3) ? 64 : 128;
+__global__ __launch_bounds__(ONE ? 256 : 512, NK <= 4 ? 4 : 2) void scores_kernel(ScoreArgs a) {
+    constexpr int kCols = ONE ? 1 : 2;                     // column tiles in work at a time
+    constexpr int kWaves = ONE ? 4 : 8, kTiles = ONE ? 1 : 2;  // row tiles of a wave
+    constexpr int kBlocks = score_blocks(ONE);
+    constexpr int DP = NK * 32, UPR = DP / 8, NP = kParts<T>;
+    // Pairs in LDS: a power of two, 64 KiB or less.
+    constexpr int kFit = 32768 / (NP * DP), kPairs = ONE ? 16 : kFit >= 256 ? 256 : kFit >= 128 ? 128 : kFit >= 64 ? 64 : 32;
     __shared__ __attribute__((aligned(16))) uint16_t qs[ONE ? 1 : kPairs * NP * DP];
-    __shared__ float kept[256];  // maxima of the chunks of pairs so far
+    __shared__ float kept[kBlocks];  // maxima of the chunks of pairs so far
     const int64_t idx = grid_index();
     if (idx >= a.items) return;
     const uint32_t rh = (uint32_t)idx / a.tile_div;
@@ -91,16 +106,16 @@ __global__ __launch_bounds__(256) void scores_kernel(ScoreArgs a) {
     const Row r = find_row(B, row);
     const int p1 = r.n > 0 ? r.p0 + r.n - 1 : -1;
     const int visible = p1 < 0 ? 0 : min(p1 / B.block + 1, B.max_blocks);
-    const int c_base = tile * 256;
+    const int c_base = tile * kBlocks;
     float *out = a.scores + ((int64_t)row * a.heads + h) * B.max_blocks;
     if (c_base >= visible) {
         const int j = c_base + (int)threadIdx.x;
-        if (j < B.max_blocks) out[j] = -kInf;
+        if (threadIdx.x < kBlocks && j < B.max_blocks) out[j] = -kInf;
         return;
     }
-    // Pages of this wave's blocks: tile i of it is blocks c_base + (4*i + wave)*16 and on.
-    const int mine = c_base + ((lane >> 4) * 4 + wave) * 16 + col;
-    const int pages = mine < visible ? page_of(B, r.b, mine) : -1;
+    // Pages of this wave's blocks: tile i of it is blocks c_base + (kWaves*i + wave)*16 and on.
+    const int mine = c_base + ((lane >> 4) * kWaves + wave) * 16 + col;
+    const int pages = lane < 16 * kTiles && mine < visible ? page_of(B, r.b, mine) : -1;
     const int pairs = r.n * a.group;
     auto query_at = [&](int m) {
         const int i = (uint32_t)m / a.group_div, g = m - i * (int)a.group_div.d;
@@ -114,8 +129,7 @@ __global__ __launch_bounds__(256) void scores_kernel(ScoreArgs a) {
     if constexpr (ONE) {
 #pragma unroll
         for (int k = 0; k < NK; ++k) {
-            const int d = k * 32 + part * 8;
-            query_parts<T>(col < pairs && d < a.dim ? load_query(query_at(col) + d, a.aligned) : none, q1[k]);
+            query_parts<T>(col < pairs ? load_part(query_at(col), k * 32, part, a.dim, a.aligned) : none, q1[k]);
         }
     }
     // Key sums of tile i, fp32.
@@ -124,13 +138,12 @@ __global__ __launch_bounds__(256) void scores_kernel(ScoreArgs a) {
         const int page = __shfl(pages, i * 16 + col);
 #pragma unroll
         for (int k = 0; k < NK; ++k) {
-            const int d = k * 32 + part * 8;
-            raw[k] = page >= 0 && d < a.dim ? load_query(a.sums + ((int64_t)page * a.heads + h) * a.dim + d, true) : none;
+            raw[k] = page >= 0 ? load_part(a.sums + ((int64_t)page * a.heads + h) * a.dim, k * 32, part, a.dim, true) : none;
         }
     };
     // Rows of a result are blocks c0 + 4*part + e, columns pairs.
     auto bounds = [&](int i, int (&key0)[4], float (&inv)[4]) {
-        const int c0 = c_base + (i * 4 + wave) * 16;
+        const int c0 = c_base + (i * kWaves + wave) * 16;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const int j = c0 + part * 4 + e;
@@ -144,83 +157,114 @@ __global__ __launch_bounds__(256) void scores_kernel(ScoreArgs a) {
         for (int o = 8; o > 0; o >>= 1)
 #pragma unroll
             for (int e = 0; e < 4; ++e) best[e] = fmaxf(best[e], __shfl_xor(best[e], o));
-        const int at = (i * 4 + wave) * 16 + part * 4 + (col & 3), j = c_base + at;
+        const int at = (i * kWaves + wave) * 16 + part * 4 + (col & 3), j = c_base + at;
         const float v = (col & 3) == 0 ? best[0] : (col & 3) == 1 ? best[1] : (col & 3) == 2 ? best[2] : best[3];
         if (col < 4) kept[at] = v;
         if (col < 4 && j < B.max_blocks) out[j] = v;
     };
 
-    const int last = (visible - c_base - wave * 16 + 63) >> 6;  // tiles of this wave that have visible blocks (0 or less: none)
-    const int tiles = min(max(last, 0), 4);
+    // Tiles of this wave that have visible blocks.
+    const int tiles = clamp_int((visible - c_base - wave * 16 + 16 * kWaves - 1) / (16 * kWaves), 0, kTiles);
     uint32_t again = 0;
     for (int m_base = 0; m_base < pairs; m_base += kPairs) {
         const int n_pairs = min(pairs - m_base, kPairs);
-        if (tiles > 0) fetch(0);
         if constexpr (!ONE) {
             __syncthreads();
-            for (int u = threadIdx.x; u < n_pairs * UPR; u += 256) {
-                const int m = u / UPR, d = (u % UPR) * 8;
+            for (int u = threadIdx.x; u < n_pairs * UPR; u += 64 * kWaves) {
+                const int m = u / UPR, k = (u % UPR) >> 2;
                 u32x4_t p[NP];
-                query_parts<T>(d < a.dim ? load_query(query_at(m_base + m) + d, a.aligned) : none, p);
+                query_parts<T>(load_part(query_at(m_base + m), k * 32, u & 3, a.dim, a.aligned), p);
 #pragma unroll
                 for (int i = 0; i < NP; ++i)
                     *reinterpret_cast<u32x4_t *>(qs + ((m * NP + i) * UPR + pair_unit<UPR>(m, u % UPR)) * 8) = p[i];
             }
             __syncthreads();
         }
+#pragma unroll 1
         for (int i = 0; i < tiles; ++i) {
-            Parts s[NK];
+            fetch(i);
+            auto split = [&](int k) {
+                Parts s;
 #pragma unroll
-            for (int k = 0; k < NK; ++k)
+                for (int e = 0; e < 4; ++e) split2(s, e, raw[k].v[2 * e], raw[k].v[2 * e + 1]);
+                return s;
+            };
+            Parts parts[ONE ? 1 : NK];
+            if constexpr (!ONE) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) split2(s[k], e, raw[k].v[2 * e], raw[k].v[2 * e + 1]);
-            if (i + 1 < tiles) fetch(i + 1);
+                for (int k = 0; k < NK; ++k) parts[k] = split(k);
+            }
             int key0[4];
-            float inv[4], best[4];
+            float inv[4], best[4] = {-kInf, -kInf, -kInf, -kInf};  // best: of the sums, before the division by the keys
             bounds(i, key0, inv);
+            const bool whole = __all(max(max(key0[0], key0[1]), max(key0[2], key0[3])) <= r.p0);  // seen by every pair
+            uint32_t largest = 0;  // magnitude's bits
+            for (int m0 = 0; m0 < n_pairs; m0 += 16 * kCols) {
+                f32x4 hi[kCols], lo[kCols];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) best[e] = m_base > 0 ? kept[(i * 4 + wave) * 16 + part * 4 + e] : -kInf;
-            bool bad = false;
-            for (int m0 = 0; m0 < n_pairs; m0 += 16) {
-                const int m = m0 + col;
-                const int p = m < n_pairs ? r.p0 + (int)((uint32_t)(m_base + m) / a.group_div) : -1;
-                f32x4 hi = {0.0f, 0.0f, 0.0f, 0.0f}, lo = {0.0f, 0.0f, 0.0f, 0.0f};
+                for (int n = 0; n < kCols; ++n) hi[n] = lo[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                 for (int k = 0; k < NK; ++k) {
-                    u32x4_t x[NP];
-                    if constexpr (ONE) {
+                    const Parts s = ONE ? split(k) : parts[ONE ? 0 : k];
+                    u32x4_t x[kCols][NP];
 #pragma unroll
-                        for (int e = 0; e < NP; ++e) x[e] = q1[k][e];
-                    } else {
+                    for (int n = 0; n < kCols; ++n)
 #pragma unroll
-                        for (int e = 0; e < NP; ++e)
-                            x[e] = *reinterpret_cast<const u32x4_t *>(qs + ((m * NP + e) * UPR + pair_unit<UPR>(m, k * 4 + part)) * 8);
-                    }
-                    hi = mma_bits(s[k].h, x[0], hi);
-                    lo = mma_bits(s[k].m, x[0], lo);
-                    lo = mma_bits(s[k].l, x[0], lo);
+                        for (int e = 0; e < NP; ++e) {
+                            const int m = m0 + n * 16 + col;
+                            if constexpr (ONE)
+                                x[n][e] = q1[k][e];
+                            else
+                                x[n][e] = *reinterpret_cast<const u32x4_t *>(
+                                    qs + ((m * NP + e) * UPR + pair_unit<UPR>(m, k * 4 + part)) * 8);
+                        }
+                    auto add = [&](f32x4 (&c)[kCols], u32x4_t s, int e) {
+#pragma unroll
+                        for (int n = 0; n < kCols; ++n) c[n] = mma_bits(s, x[n][e], c[n]);
+                    };
+                    add(lo, s.m, 0);
+                    add(hi, s.h, 0);
+                    add(lo, s.l, 0);
                     if constexpr (NP > 1) {
-                        lo = mma_bits(s[k].h, x[1], lo);
-                        lo = mma_bits(s[k].m, x[1], lo);
+                        add(lo, s.h, 1);
+                        add(lo, s.m, 1);
                     }
-                    if constexpr (NP > 2) lo = mma_bits(s[k].h, x[2], lo);
+                    if constexpr (NP > 2) add(lo, s.h, 2);
                 }
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float v = (hi[e] + lo[e]) * inv[e];
-                    if (p >= key0[e]) {
-                        bad = bad || !(fabsf(v) < kInf);
-                        best[e] = fmaxf(best[e], v);
+                for (int n = 0; n < kCols; ++n) {
+                    f32x4 v = hi[n] + lo[n];
+                    if (whole && m0 + n * 16 + 16 <= n_pairs) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            best[e] = fmaxf(best[e], v[e]);
+                            largest = max(largest, __float_as_uint(v[e]) & 0x7fffffffu);
+                        }
+                    } else {
+                        const int m = m0 + n * 16 + col;
+                        const int p = m < n_pairs ? r.p0 + (int)((uint32_t)(m_base + m) / a.group_div) : -1;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const bool seen = p >= key0[e];
+                            best[e] = fmaxf(best[e], seen ? v[e] : -kInf);
+                            largest = max(largest, seen ? __float_as_uint(v[e]) & 0x7fffffffu : 0u);
+                        }
                     }
                 }
             }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                best[e] *= inv[e];
+                if (m_base > 0) best[e] = fmaxf(best[e], kept[(i * kWaves + wave) * 16 + part * 4 + e]);
+            }
+            const bool bad = largest >= 0x7f800000u;
             if (__ballot(bad)) again |= 1u << i;
             finish(i, best);
         }
         // Tiles of this wave behind the visible blocks.
         if (m_base == 0)
-            for (int i = tiles; i < 4; ++i) {
-                const int j = c_base + (i * 4 + wave) * 16 + lane;
+            for (int i = tiles; i < kTiles; ++i) {
+                const int j = c_base + (i * kWaves + wave) * 16 + lane;
                 if (lane < 16 && j < B.max_blocks) out[j] = -kInf;
             }
     }
@@ -237,8 +281,7 @@ __global__ __launch_bounds__(256) void scores_kernel(ScoreArgs a) {
             f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int k = 0; k < NK; ++k) {
-                const int d = k * 32 + part * 8;
-                const Floats<8> x = p >= 0 && d < a.dim ? load_query(query_at(m) + d, a.aligned) : none;
+                const Floats<8> x = p >= 0 ? load_part(query_at(m), k * 32, part, a.dim, a.aligned) : none;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(raw[k].v[e], x.v[e], acc, 0, 0, 0);
             }
@@ -288,11 +331,13 @@ __device__ __forceinline__ Choice choice_of(const SelectArgs &a, const Row &r) {
 // One wave a (row, head) of at most 64*NI blocks, held in registers: the want-th highest
 // value of the candidates is found bit by bit from the top, by counting those that
 // are not below a trial, until exactly `want` are left or the bits are through (ties:
-// the lowest indices of those equal to it). Then the list is written in order.
+// the lowest indices of those equal to it). As soon as 64 or less can still be it, they are
+// put into one register, and a count is one instruction instead of NI (a compare, a count
+// and an addition each: 512 blocks would take 32 times 24 of these). Then the list is written in order.
 template <int NI>
 __global__ __launch_bounds__(256) void select_wave_kernel(SelectArgs a) {
     const int lane = threadIdx.x & 63;
-    const int64_t item = grid_index() * 4 + (threadIdx.x >> 6);
+    const int64_t item = grid_index() * 4 + uniform((int)(threadIdx.x >> 6));
     if (item >= a.items) return;
     const int row = (int)((uint32_t)item / a.head_div);
     const Row r = find_row(a.B, row);
@@ -304,17 +349,25 @@ __global__ __launch_bounds__(256) void select_wave_kernel(SelectArgs a) {
         for (int i = lane; i < a.keep; i += 64) blocks[i] = i < c.n ? i : -1;
         return;
     }
+    __shared__ uint32_t lists[4][64];
     const float *s = a.scores + item * a.B.max_blocks;
     uint32_t v[NI];
+    {
+        float x[NI];  // all loads on their way before the first is looked at
 #pragma unroll
-    for (int i = 0; i < NI; ++i) {
-        const int j = i * 64 + lane;
-        v[i] = j >= c.sink && j < c.low ? order_of(s[j]) : 0u;
+        for (int i = 0; i < NI; ++i) x[i] = s[min(i * 64 + lane, c.n - 1)];
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+            const int j = i * 64 + lane;
+            v[i] = j >= c.sink && j < c.low ? order_of(x[i]) : 0u;
+        }
     }
-    uint32_t cut = 0;  // highest t with want or more candidates >= t
-    int above = -1;    // exactly want candidates are >= cut, once known
+    uint32_t cut = 0;       // highest t with want or more candidates >= t
+    int above = c.low - c.sink, over = 0;  // candidates >= cut, and of those that are out of question: >= the lowest t with less than want
     if (c.want > 0) {
-        for (int bit = 31; bit >= 0; --bit) {
+        uint32_t top = 0;   // that t; 0: none yet
+        int bit = 31;
+        for (; bit >= 0 && above != c.want && above - over > 64; --bit) {
             const uint32_t t = cut | (1u << bit);
             int n = 0;
 #pragma unroll
@@ -322,7 +375,30 @@ __global__ __launch_bounds__(256) void select_wave_kernel(SelectArgs a) {
             if (n >= c.want) {
                 cut = t;
                 above = n;
-                if (n == c.want) break;
+            } else {
+                top = t;
+                over = n;
+            }
+        }
+        if (bit >= 0 && above != c.want) {
+            uint32_t *few = lists[threadIdx.x >> 6];
+            int at = 0;
+#pragma unroll
+            for (int i = 0; i < NI; ++i) {
+                const bool in = v[i] >= cut && v[i] != 0u && (top == 0u || v[i] < top);
+                const uint64_t all = __ballot(in);
+                if (in) few[at + bits(all & ((1ull << lane) - 1))] = v[i];
+                at += bits(all);
+            }
+            __builtin_amdgcn_wave_barrier();
+            const uint32_t x = lane < at ? few[lane] : 0u;
+            for (; bit >= 0 && above != c.want; --bit) {
+                const uint32_t t = cut | (1u << bit);
+                const int n = over + bits(__ballot(x >= t));
+                if (n >= c.want) {
+                    cut = t;
+                    above = n;
+                }
             }
         }
     }
@@ -443,12 +519,13 @@ __global__ __launch_bounds__(1024) void select_block_kernel(SelectArgs a, int pe
 template <typename T, bool ONE>
 int scores_of(const ScoreArgs &a, hipStream_t stream) {
     const dim3 grid = grid_of(a.items);
+    constexpr int threads = ONE ? 256 : 512;
     if (a.dim <= 64)
-        scores_kernel<T, 2, ONE><<<grid, 256, 0, stream>>>(a);
+        scores_kernel<T, 2, ONE><<<grid, threads, 0, stream>>>(a);
     else if (a.dim <= 128)
-        scores_kernel<T, 4, ONE><<<grid, 256, 0, stream>>>(a);
+        scores_kernel<T, 4, ONE><<<grid, threads, 0, stream>>>(a);
     else
-        scores_kernel<T, 8, ONE><<<grid, 256, 0, stream>>>(a);
+        scores_kernel<T, 8, ONE><<<grid, threads, 0, stream>>>(a);
     return launched();
 }
 
@@ -465,7 +542,8 @@ extern "C" int spconv_block_scores(int dtype, const spconv_batch *batch, const v
     if (!batch_ok(batch) || !batch_arrays_ok(batch) || !dtype_ok(dtype) || q == nullptr || sums == nullptr ||
         scores == nullptr || !heads_ok(q_heads, heads, dim) || q_token < 0 || q_head < 0 || !aligned16(sums))
         return SPCONV_EINVAL;
-    const int tiles = (batch->max_blocks + 255) / 256;
+    const int per = score_blocks((int64_t)batch->q_block * (q_heads / std::max(heads, 1)) <= 16);
+    const int tiles = (batch->max_blocks + per - 1) / per;
     const int64_t rows = rows_of(batch);
     if (rows * heads * tiles >= ((int64_t)1 << 31)) return SPCONV_EINVAL;
     ScoreArgs a{*batch, q, q_token, q_head, sums, scores, rows * heads * tiles, heads, q_heads / heads, dim, tiles,
