@@ -299,13 +299,14 @@ struct SelectArgs {
     int32_t *blocks, *counts;
     int64_t items;  // rows * heads
     int heads, keep, sink, local;
+    int each;       // items a wave takes
     Div head_div;
 };
 
-// Order of the values as unsigned numbers: 0 stands for "no candidate", -infinity
-// and NaN are 1 (the map of -infinity is 0x007fffff), -0 is +0.
+// Order of the values as unsigned numbers: 0 stands for "no candidate", NaN counts as -infinity
+// (0x007fffff), -0 as +0.
 __device__ __forceinline__ uint32_t order_of(float x) {
-    if (!(x > -kInf)) return 1u;
+    if (!(x > -kInf)) return 0x007fffffu;
     const uint32_t u = __float_as_uint(x + 0.0f);
     return (u & 0x80000000u) ? ~u : u | 0x80000000u;
 }
@@ -328,20 +329,38 @@ __device__ __forceinline__ Choice choice_of(const SelectArgs &a, const Row &r) {
     return c;
 }
 
-// One wave a (row, head) of at most 64*NI blocks, held in registers: the want-th highest
-// value of the candidates is found bit by bit from the top, by counting those that
-// are not below a trial, until exactly `want` are left or the bits are through (ties:
-// the lowest indices of those equal to it). As soon as 64 or less can still be it, they are
-// put into one register, and a count is one instruction instead of NI (a compare, a count
-// and an addition each: 512 blocks would take 32 times 24 of these). Then the list is written in order.
+// The value whose order is u (not that of NaN).
+__device__ __forceinline__ float value_of(uint32_t u) { return __uint_as_float((u & 0x80000000u) ? u & 0x7fffffffu : ~u); }
+
+// Ones of a ballot in the lanes below this one.
+__device__ __forceinline__ int before(uint64_t x) {
+    return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(x >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)x, 0));
+}
+
+// Maximum over the wave: neighbours 1, 2, 4 and 8 lanes back in each row of 16, then the last lanes of the rows
+// before; lane 63 has it all.
+__device__ __forceinline__ float wave_max(float x) {
+    auto step = [&](float v) { x = fmaxf(x, v); };
+#define SPCONV_DPP(ctrl) \
+    step(__int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(x), __float_as_int(x), ctrl, 0xf, 0xf, false)))
+    SPCONV_DPP(0x111);
+    SPCONV_DPP(0x112);
+    SPCONV_DPP(0x114);
+    SPCONV_DPP(0x118);
+    SPCONV_DPP(0x142);
+    SPCONV_DPP(0x143);
+#undef SPCONV_DPP
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
+}
+
+// One (row, head) of at most 64*NI blocks by one wave, held in registers. Bound by instructions (a count over all
+// values is 3*NI of them), so few counts are taken: a lower bound from the lanes' highest values, or halving the range
+// of the values, soon leaves 64 or less that can be the want-th highest (many equal or infinite
+// ones end at the most steps, and then the range of their order is halved). Those go to one register, where a count
+// is one instruction, and the search ends there, by trying one of them after another (log2 of them or so). Of the
+// want-th highest's equals the lowest indices are taken. Then the list is written in order.
 template <int NI>
-__global__ __launch_bounds__(256) void select_wave_kernel(SelectArgs a) {
-    const int lane = threadIdx.x & 63;
-    const int64_t item = grid_index() * 4 + uniform((int)(threadIdx.x >> 6));
-    if (item >= a.items) return;
-    const int row = (int)((uint32_t)item / a.head_div);
-    const Row r = find_row(a.B, row);
-    const Choice c = choice_of(a, r);
+__device__ __forceinline__ void select_row(const SelectArgs &a, const Choice &c, int64_t item, int lane, float *few) {
     int32_t *blocks = a.blocks + item * a.keep;
     const int count = min(c.n, a.keep);
     if (lane == 0) a.counts[item] = count;
@@ -349,85 +368,148 @@ __global__ __launch_bounds__(256) void select_wave_kernel(SelectArgs a) {
         for (int i = lane; i < a.keep; i += 64) blocks[i] = i < c.n ? i : -1;
         return;
     }
-    __shared__ uint32_t lists[4][64];
     const float *s = a.scores + item * a.B.max_blocks;
-    uint32_t v[NI];
-    {
-        float x[NI];  // all loads on their way before the first is looked at
+    // Candidates' values; NaN, which no comparison finds, for blocks that are none.
+    float v[NI];
 #pragma unroll
-        for (int i = 0; i < NI; ++i) x[i] = s[min(i * 64 + lane, c.n - 1)];
+    for (int i = 0; i < NI; ++i) v[i] = s[min(i * 64 + lane, c.n - 1)];
+    float mine = __builtin_nanf("");  // this lane's highest
 #pragma unroll
-        for (int i = 0; i < NI; ++i) {
-            const int j = i * 64 + lane;
-            v[i] = j >= c.sink && j < c.low ? order_of(x[i]) : 0u;
-        }
+    for (int i = 0; i < NI; ++i) {
+        const int j = i * 64 + lane;
+        v[i] = v[i] > -kInf ? v[i] : -kInf;  // NaN counts as -infinity
+        v[i] = j >= c.sink && j < c.low ? v[i] : __builtin_nanf("");
+        mine = fmaxf(mine, v[i]);
     }
-    uint32_t cut = 0;       // highest t with want or more candidates >= t
-    int above = c.low - c.sink, over = 0;  // candidates >= cut, and of those that are out of question: >= the lowest t with less than want
+    float cut = __builtin_nanf("");  // what is not below it is taken: none without candidates to choose
+    int ties = 0x7fffffff;           // and of those equal to it so many
     if (c.want > 0) {
-        uint32_t top = 0;   // that t; 0: none yet
-        int bit = 31;
-        for (; bit >= 0 && above != c.want && above - over > 64; --bit) {
-            const uint32_t t = cut | (1u << bit);
+        auto not_below = [&](float t) {
             int n = 0;
 #pragma unroll
             for (int i = 0; i < NI; ++i) n += bits(__ballot(v[i] >= t));
+            return n;
+        };
+        // want or more are not below lo, less are not below hi (from above the maximum on).
+        const float most = wave_max(mine);
+        float hi = most, lo = -kInf;
+        int at_lo = c.low - c.sink, at_hi = 0;
+        // A value that want or a few more lanes' highest reach is not far below the want-th highest of all.
+        if (c.want < bits(__ballot(mine > -kInf))) {
+            lo = -wave_max(-mine);
+            for (int i = 0; i < 8; ++i) {
+                const float t = 0.5f * lo + 0.5f * hi;
+                const int n = bits(__ballot(mine >= t));
+                if (n >= c.want) lo = t;
+                else hi = t;
+                if (n >= c.want && n <= c.want + 4) break;
+            }
+            hi = most;
+            at_lo = not_below(lo);
+        }
+        bool open = true;  // hi is the maximum, and may be the one
+        for (int i = 0; i < 10 && at_lo != c.want && at_lo - at_hi > 64; ++i) {
+            const float t = 0.5f * lo + 0.5f * hi;
+            if (!(t > lo && t < hi)) break;
+            const int n = not_below(t);
             if (n >= c.want) {
-                cut = t;
-                above = n;
+                lo = t;
+                at_lo = n;
             } else {
-                top = t;
-                over = n;
+                hi = t;
+                at_hi = n;
+                open = false;
             }
         }
-        if (bit >= 0 && above != c.want) {
-            uint32_t *few = lists[threadIdx.x >> 6];
+        uint32_t a0 = order_of(lo), a1 = order_of(hi) + (open ? 1u : 0u);  // the same in orders: [a0, a1)
+        while (at_lo != c.want && at_lo - at_hi > 64 && a1 - a0 > 1) {
+            const uint32_t t = a0 + (a1 - a0) / 2;
+            const int n = not_below(value_of(t));
+            if (n >= c.want) {
+                a0 = t;
+                at_lo = n;
+            } else {
+                a1 = t;
+                at_hi = n;
+                open = false;
+            }
+        }
+        if (at_lo != c.want && a1 - a0 > 1) {
+            const float from = value_of(a0), to = open ? __builtin_nanf("") : value_of(a1);
             int at = 0;
 #pragma unroll
             for (int i = 0; i < NI; ++i) {
-                const bool in = v[i] >= cut && v[i] != 0u && (top == 0u || v[i] < top);
+                const bool in = v[i] >= from && !(v[i] >= to);
                 const uint64_t all = __ballot(in);
-                if (in) few[at + bits(all & ((1ull << lane) - 1))] = v[i];
+                few[in ? at + before(all) : 64] = v[i];  // (behind the list: what is not in it)
                 at += bits(all);
             }
             __builtin_amdgcn_wave_barrier();
-            const uint32_t x = lane < at ? few[lane] : 0u;
-            for (; bit >= 0 && above != c.want; --bit) {
-                const uint32_t t = cut | (1u << bit);
-                const int n = over + bits(__ballot(x >= t));
-                if (n >= c.want) {
+            const float x = lane < at ? few[lane] : __builtin_nanf("");
+            // One of those that can still be it at a time: with how many are above it and equal to it, it is the one or
+            // leaves those on one side.
+            uint64_t left = __ballot(lane < at);
+            while (left != 0) {
+                const float t = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), __builtin_ctzll(left)));
+                const uint64_t gt = __ballot(x > t), ge = __ballot(x >= t);
+                if (at_hi + bits(gt) >= c.want) {
+                    left &= gt;
+                } else if (at_hi + bits(ge) < c.want) {
+                    left &= ~ge;
+                } else {
                     cut = t;
-                    above = n;
+                    at_lo = at_hi + bits(ge);
+                    at_hi += bits(gt);
+                    break;
                 }
             }
+        } else {
+            cut = value_of(a0);
         }
-    }
-    // Of those equal to the cut, how many are taken (all, if exactly want are not below it).
-    int ties = 0x7fffffff;
-    if (c.want <= 0) {
-        cut = 0xffffffffu;
-        ties = 0;
-    } else if (above != c.want) {
-        int n = 0;
-#pragma unroll
-        for (int i = 0; i < NI; ++i) n += bits(__ballot(v[i] > cut));
-        ties = c.want - n;
+        if (at_lo != c.want) ties = c.want - at_hi;  // the cut is the want-th highest, at_hi are above it
     }
     int at = 0;
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
+        if (i * 64 >= c.n) break;
         const int j = i * 64 + lane;
-        const uint64_t below = (1ull << lane) - 1;
-        const uint64_t eq = __ballot(v[i] == cut);
-        const bool tie = v[i] == cut && bits(eq & below) < ties;
-        const bool take = j < c.n && (j < c.sink || j >= c.low || v[i] > cut || tie);
-        if (ties != 0x7fffffff) ties = max(0, ties - bits(eq));
+        bool take = v[i] >= cut;
+        if (ties != 0x7fffffff) {
+            const uint64_t eq = __ballot(v[i] == cut);
+            take = take && !(v[i] == cut && before(eq) >= ties);
+            ties = max(0, ties - bits(eq));
+        }
+        if (i * 64 < c.sink || i * 64 + 64 > c.low) take = j < c.n && (take || j < c.sink || j >= c.low);
         const uint64_t all = __ballot(take);
-        const int pos = at + bits(all & below);
+        const int pos = at + before(all);
         if (take && pos < a.keep) blocks[pos] = j;
         at += bits(all);
     }
     for (int i = at + lane; i < a.keep; i += 64) blocks[i] = -1;
+}
+
+// One wave `each` neighbouring (row, head): where there are more of them than waves on the GPU, a row is looked up
+// once for several of its heads.
+template <int NI>
+__global__ __launch_bounds__(256) void select_wave_kernel(SelectArgs a) {
+    __shared__ float lists[4][65];
+    const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6));
+    const int64_t first = (grid_index() * 4 + wave) * a.each, end = min(first + a.each, a.items);
+    if (first >= a.items) return;
+    Row r;
+    Choice c;
+    int row = -1;
+    for (int64_t item = first; item < end; ++item) {
+        if ((int)((uint32_t)item / a.head_div) != row) {
+            row = (int)((uint32_t)item / a.head_div);
+            r = find_row(a.B, row);
+            c = choice_of(a, r);
+        }
+        if (NI > 4 && c.n <= NI * 32)
+            select_row<NI / 2>(a, c, item, lane, lists[wave]);
+        else
+            select_row<NI>(a, c, item, lane, lists[wave]);
+    }
 }
 
 // One workgroup of 1024 threads a (row, head) of more blocks: wave w takes the w-th
@@ -562,10 +644,11 @@ extern "C" int spconv_select_blocks(const spconv_batch *batch, int heads, const 
     const int64_t always = (int64_t)sink + local + (batch->q_block - 1 + batch->block - 1) / batch->block;
     const int64_t items = rows_of(batch) * heads;
     if (keep < always || items >= ((int64_t)1 << 31) || items * keep >= ((int64_t)1 << 40)) return SPCONV_EINVAL;
-    SelectArgs a{*batch, scores, blocks, counts, items, heads, keep, sink, local, make_div((uint32_t)heads)};
+    SelectArgs a{*batch, scores, blocks, counts, items, heads, keep, sink, local, 1, make_div((uint32_t)heads)};
     const int n = (batch->max_blocks + 63) / 64;
     if (n <= 32) {
-        const dim3 grid = grid_of((items + 3) / 4);
+        a.each = (int)std::min<int64_t>(std::max<int64_t>(items / 8192, 1), heads);  // 8192 waves fill the GPU
+        const dim3 grid = grid_of(((items + a.each - 1) / a.each + 3) / 4);
         if (n <= 4)
             select_wave_kernel<4><<<grid, 256, 0, stream>>>(a);
         else if (n <= 8)
