@@ -30,18 +30,22 @@ struct Floats {
 };
 
 template <typename T, int W>
-__device__ __forceinline__ Floats<W> load_floats(const T *p) {
+__device__ __forceinline__ Floats<W> floats_of(typename VecOf<T, W>::type v) {
     Floats<W> r;
     if constexpr (W == 1) {
-        r.v[0] = (float)*p;
+        r.v[0] = (float)v;
     } else {
-        typedef typename VecOf<T, W>::type V;
         typedef typename VecOf<float, W>::type F;
-        const F f = __builtin_convertvector(*reinterpret_cast<const V *>(p), F);
+        const F f = __builtin_convertvector(v, F);
 #pragma unroll
         for (int i = 0; i < W; ++i) r.v[i] = f[i];
     }
     return r;
+}
+
+template <typename T, int W>
+__device__ __forceinline__ Floats<W> load_floats(const T *p) {
+    return floats_of<T, W>(*reinterpret_cast<const typename VecOf<T, W>::type *>(p));
 }
 
 // Rounds (to nearest even) and stores W elements; what was stored comes back.

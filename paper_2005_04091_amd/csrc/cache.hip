@@ -122,24 +122,33 @@ struct AppendArgs {
     float *sums;
     const int32_t *positions;
     const double *freq;
-    int64_t items;
+    int64_t items;  // touched pages
     int heads, dim, rot;
-    Div units;  // vectors of a key (pairs and copies)
-    Div vecs;   // vectors of a value
+    int each;       // heads that a workgroup takes one after another
+    int rows;       // rows of a page whose sines fit the table at a time
+    int table_len;
+    Div head_groups, half, units, vecs;  // heads / each; rot/2; vectors of a key (pairs and copies); vectors of a value
     float amplitude;
 };
 
-// One workgroup a (touched page, head). The pages that sequence b touches are items
+constexpr int kTable = 4096;  // sines and cosines in LDS at most
+
+// One workgroup a (touched page, group of heads). The pages that sequence b touches are items
 // q_start[b]/block + 2b and on: a sequence of n tokens touches n/block + 2 pages at
-// most. Threads hold one vector pair of a key each and walk the page's rows
-// in strides, so that the page's sum is a sum of a thread's rows and then of 256/units
-// threads, always in the same order: no atomics.
+// most. Sines and cosines of the page's new tokens are formed once for the group's heads, in LDS. Threads hold one
+// vector pair of a key each and walk the page's rows in strides, so that the
+// page's sum is a sum of a thread's rows and then of 256/units threads, always in the same order: no atomics.
+// Bound by HBM where the page is new; single tokens read the page's older keys, for the sum, and are bound by
+// the latency of length, page and keys one after another.
 template <typename T, int W, bool INTER>
 __global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
-    __shared__ float part[256 * 2 * W];
-    const int64_t item = grid_index() / a.heads;
-    const int h = (int)(grid_index() - item * a.heads);
-    if (item >= a.items) return;
+    extern __shared__ CosSin table[];                             // sines of the new rows, then
+    float *part = reinterpret_cast<float *>(table + a.table_len);  // [groups][dim] partial sums
+    typedef typename VecOf<T, W>::type V;
+    const int64_t idx = grid_index();
+    if (idx >= a.items * a.head_groups.d) return;
+    const uint32_t item = (uint32_t)idx / a.head_groups;
+    const int h0 = (int)((uint32_t)idx - item * a.head_groups.d) * a.each;
     const spconv_batch &B = a.B;
     const Seq s = find_seq(B, (int)item, B.block, 2);
     if (s.b < 0 || s.at < 0 || s.n == 0 || s.kv == 0) return;
@@ -147,29 +156,12 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
     const int64_t block64 = max(from, 0) / B.block + (int64_t)s.at;
     if (block64 > (s.kv - 1) / B.block) return;
     const int j = (int)block64;
-    const int page = page_of(B, s.b, j);
+    const int page = uniform(page_of(B, s.b, j));
     if (page < 0) return;
     const int s0 = max(from - j * B.block, 0), s1 = min(s.kv - j * B.block, B.block);
     const int t_off = s.first + j * B.block - from;  // token of slot s: s + t_off
     const int tid = threadIdx.x;
-    const int64_t base = ((int64_t)page * a.heads + h) * B.block * a.dim;
-    T *kc = (T *)a.k_cache + base, *vc = (T *)a.v_cache + base;
 
-    // Values: copied.
-    const int nv = (s1 - s0) * (int)a.vecs.d;
-    for (int i = tid; i < nv; i += 256) {
-        const int r = (uint32_t)i / a.vecs, c = (i - r * (int)a.vecs.d) * W;
-        const T *src = (const T *)a.v + (int64_t)(s0 + r + t_off) * a.v_token + h * a.v_head + c;
-        T *dst = vc + (int64_t)(s0 + r) * a.dim + c;
-        if constexpr (W == 1) {
-            *dst = *src;
-        } else {
-            typedef typename VecOf<T, W>::type V;
-            *reinterpret_cast<V *>(dst) = *reinterpret_cast<const V *>(src);
-        }
-    }
-
-    // Keys: rotated, stored, summed.
     const int units = a.units.d, groups = 256 / units;
     const int g = (uint32_t)tid / a.units, u = tid - g * units;
     const bool pair = u * W < a.rot / 2;
@@ -178,55 +170,75 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
         pair_at<W, INTER>(u, a.rot, d0, d1);
     else
         d0 = a.rot / 2 + u * W;
-    Floats<W> sum0, sum1;
+
+    auto angles = [&](int r0, int r1) {  // of slots [r0, r1)
+        for (int i = tid; i < (r1 - r0) * (a.rot / 2); i += 256) {
+            const int r = (uint32_t)i / a.half, t = r0 + r + t_off;
+            table[i] = rope_angle(a.positions ? a.positions[t] : j * B.block + r0 + r, a.freq[i - r * (int)a.half.d], 1.0f,
+                                  a.amplitude);
+        }
+    };
+    const bool once = s1 - s0 <= a.rows;
+    if (once) angles(s0, s1);
+    for (int h = h0; h < min(h0 + a.each, a.heads); ++h) {
+        const int64_t base = ((int64_t)page * a.heads + h) * B.block * a.dim;
+        T *kc = (T *)a.k_cache + base, *vc = (T *)a.v_cache + base;
+        // Values: copied.
+        const int nv = (s1 - s0) * (int)a.vecs.d;
+        for (int i = tid; i < nv; i += 256) {
+            const int r = (uint32_t)i / a.vecs, c = (i - r * (int)a.vecs.d) * W;
+            *reinterpret_cast<V *>(vc + (int64_t)(s0 + r) * a.dim + c) =
+                *reinterpret_cast<const V *>((const T *)a.v + (int64_t)(s0 + r + t_off) * a.v_token + h * a.v_head + c);
+        }
+        // Keys: rotated, stored, summed, older ones only summed; as many new rows at a time as the table holds.
+        Floats<W> sum0, sum1;
 #pragma unroll
-    for (int i = 0; i < W; ++i) sum0.v[i] = sum1.v[i] = 0.0f;
-    if (g < groups) {
-        const int r0 = a.sums ? 0 : s0;
-        for (int r = r0 + g; r < s1; r += groups) {
-            T *dst = kc + (int64_t)r * a.dim;
-            Floats<W> p, q;
-#pragma unroll
-            for (int i = 0; i < W; ++i) q.v[i] = 0.0f;
-            if (r < s0) {
-                p = load_floats<T, W>(dst + d0);
-                if (pair) q = load_floats<T, W>(dst + d1);
-            } else {
-                const int t = r + t_off;
-                const T *src = (const T *)a.k + (int64_t)t * a.k_token + h * a.k_head;
-                p = load_floats<T, W>(src + d0);
-                if (pair) {
-                    q = load_floats<T, W>(src + d1);
-                    const int position = a.positions ? a.positions[t] : j * B.block + r;
-                    CosSin m[W];
-#pragma unroll
-                    for (int k = 0; k < W; ++k) m[k] = rope_angle(position, a.freq[u * W + k], 1.0f, a.amplitude);
-                    rotate<W, INTER>(p, q, m);
-                    q = store_floats<T, W>(dst + d1, q);
-                }
-                p = store_floats<T, W>(dst + d0, p);
+        for (int i = 0; i < W; ++i) sum0.v[i] = sum1.v[i] = 0.0f;
+        for (int n0 = s0; n0 < s1; n0 += a.rows) {
+            const int n1 = min(n0 + a.rows, s1);
+            if (!once) {
+                __syncthreads();
+                angles(n0, n1);
             }
+            __syncthreads();
+            if (g >= groups) continue;
+            for (int r = (n0 > s0 ? n0 : a.sums ? 0 : s0) + g; r < n1; r += groups) {
+                T *dst = kc + (int64_t)r * a.dim;
+                const T *src = r < s0 ? dst : (const T *)a.k + (int64_t)(r + t_off) * a.k_token + h * a.k_head;
+                Floats<W> p = load_floats<T, W>(src + d0), q = load_floats<T, W>(src + (pair ? d1 : d0));
+                if (r >= s0) {
+                    if (pair) {
+                        CosSin m[W];
+#pragma unroll
+                        for (int k = 0; k < W; ++k) m[k] = table[(r - n0) * (int)a.half.d + u * W + k];
+                        rotate<W, INTER>(p, q, m);
+                        q = store_floats<T, W>(dst + d1, q);
+                    }
+                    p = store_floats<T, W>(dst + d0, p);
+                }
+#pragma unroll
+                for (int i = 0; i < W; ++i) {
+                    sum0.v[i] += p.v[i];
+                    sum1.v[i] += q.v[i];  // (of a copied vector: not used)
+                }
+            }
+        }
+        if (a.sums == nullptr) continue;
+        if (g < groups) {
 #pragma unroll
             for (int i = 0; i < W; ++i) {
-                sum0.v[i] += p.v[i];
-                sum1.v[i] += q.v[i];
+                part[g * a.dim + d0 + i] = sum0.v[i];
+                if (pair) part[g * a.dim + d1 + i] = sum1.v[i];
             }
         }
-    }
-    if (a.sums == nullptr) return;
-    if (g < groups) {
-#pragma unroll
-        for (int i = 0; i < W; ++i) {
-            part[g * a.dim + d0 + i] = sum0.v[i];
-            if (pair) part[g * a.dim + d1 + i] = sum1.v[i];
+        __syncthreads();
+        float *sums = a.sums + ((int64_t)page * a.heads + h) * a.dim;
+        for (int d = tid; d < a.dim; d += 256) {
+            float t = 0.0f;
+            for (int k = 0; k < groups; ++k) t += part[k * a.dim + d];
+            sums[d] = t;
         }
-    }
-    __syncthreads();
-    float *sums = a.sums + ((int64_t)page * a.heads + h) * a.dim;
-    for (int d = tid; d < a.dim; d += 256) {
-        float t = 0.0f;
-        for (int k = 0; k < groups; ++k) t += part[k * a.dim + d];
-        sums[d] = t;
+        __syncthreads();
     }
 }
 
@@ -266,11 +278,18 @@ template <typename T, int W>
 int launch_append(AppendArgs &a, bool inter, hipStream_t stream) {
     a.units = make_div((uint32_t)((a.dim - a.rot / 2) / W));
     a.vecs = make_div((uint32_t)(a.dim / W));
-    const dim3 grid = grid_of(a.items * a.heads);
+    a.half = make_div((uint32_t)std::max(a.rot / 2, 1));
+    a.rows = std::min(kTable / std::max(a.rot / 2, 1), a.B.q_start ? a.B.block : 1);
+    a.table_len = a.rows * (a.rot / 2);
+    const size_t lds = a.table_len * sizeof(CosSin) + (a.sums ? 256 / a.units.d * a.dim * sizeof(float) : 0);
+    // Heads a workgroup takes: as many as leave eight workgroups for every CU.
+    a.each = (int)std::min<int64_t>(std::max<int64_t>(a.items * a.heads / 2048, 1), a.heads);
+    a.head_groups = make_div((uint32_t)((a.heads + a.each - 1) / a.each));
+    const dim3 grid = grid_of(a.items * a.head_groups.d);
     if (inter)
-        append_kernel<T, W, true><<<grid, 256, 0, stream>>>(a);
+        append_kernel<T, W, true><<<grid, 256, lds, stream>>>(a);
     else
-        append_kernel<T, W, false><<<grid, 256, 0, stream>>>(a);
+        append_kernel<T, W, false><<<grid, 256, lds, stream>>>(a);
     return launched();
 }
 
@@ -351,9 +370,9 @@ extern "C" int spconv_cache_append(int dtype, const spconv_batch *batch, const v
     // Touched pages of all sequences; one each without q_start.
     const int64_t items =
         batch->q_start ? batch->tokens / batch->block + 2 * (int64_t)batch->sequences : (int64_t)batch->sequences;
-    if (items > 0x7fffffff) return SPCONV_EINVAL;
+    if (items * heads > 0x7fffffff) return SPCONV_EINVAL;
     AppendArgs a{*batch, k, v, k_token, k_head, v_token, v_head, k_cache, v_cache, sums, positions, freq, items, heads,
-                 dim, rot, {}, {}, amplitude};
+                 dim, rot, 1, 1, 0, {}, {}, {}, {}, amplitude};
     const bool inter = (flags & SPCONV_ROPE_INTERLEAVED) != 0;
     if (dtype == SPCONV_F32) return append_of<float>(a, inter, stream);
     if (dtype == SPCONV_F16) return append_of<_Float16>(a, inter, stream);
