@@ -13,6 +13,8 @@ last is 1; caches are [pages, heads, block, dim], key sums [pages, heads, dim].
 from __future__ import annotations
 
 import ctypes
+from contextlib import contextmanager
+from functools import lru_cache
 
 import numpy as np
 import torch
@@ -116,27 +118,37 @@ def _dims3(t, name):
     return t.shape
 
 
-class _On:
-    """The device a call runs on made current, and its raw stream (torch's current one without ``stream``).
-    Outputs and scratch memory are allocated inside, so that they belong to that stream."""
+class _Here:
+    """A call on the current device and its current stream: nothing to switch."""
+    __slots__ = ("_raw",)
 
-    def __init__(self, device, stream):
-        self._contexts = []
-        if device.index != torch.cuda.current_device():
-            self._contexts.append(torch.cuda.device(device))
-        if stream is not None:
-            self._contexts.append(torch.cuda.stream(stream))
-        self._device, self._stream = device, stream
+    def __init__(self, raw):
+        self._raw = raw
 
     def __enter__(self):
-        for c in self._contexts:
-            c.__enter__()
-        return (self._stream or torch.cuda.current_stream(self._device)).cuda_stream
+        return self._raw
 
     def __exit__(self, *exc):
-        for c in reversed(self._contexts):
-            c.__exit__(*exc)
         return False
+
+
+@contextmanager
+def _elsewhere(device, stream):
+    with torch.cuda.device(device):
+        if stream is None:
+            yield torch.cuda.current_stream(device).cuda_stream
+        else:
+            with torch.cuda.stream(stream):
+                yield stream.cuda_stream
+
+
+def _on(device, stream):
+    """The device a call runs on made current, and its raw stream (torch's current one without ``stream``).
+    Outputs and scratch memory are allocated inside, so that they belong to that stream."""
+    # (The usual case asks torch for two numbers: its Python classes for them take 4 us, as long as a launch.)
+    if stream is None and device.index == torch._C._cuda_getDevice():
+        return _Here(torch._C._cuda_getCurrentRawStream(device.index))
+    return _elsewhere(device, stream)
 
 
 class CacheBatch:
@@ -160,18 +172,17 @@ class CacheBatch:
             raise ValueError("a batch with q_start needs the number of tokens")
         self.table, self.kv_len, self.q_start = table, kv_len, q_start  # kept alive
         self.sequences, self.max_blocks, self.block, self.q_block, self.tokens = B, nb, block, q_block, tokens
-        # One page until a call knows the cache.
-        self.struct = spconv_batch(B, block, nb, q_block, tokens, 1, stride, table.data_ptr(), kv_len.data_ptr(),
-                                   None if q_start is None else q_start.data_ptr())
+        self._fields = (B, block, nb, q_block, tokens, stride, table.data_ptr(), kv_len.data_ptr(),
+                        None if q_start is None else q_start.data_ptr())
+        self.struct = self.with_pages(1)  # until a call knows the cache
         rows = _i64()
         _check(_lib.spconv_batch_rows(self.struct, rows), "spconv_batch_rows")
         self.rows = rows.value
 
     def with_pages(self, pages: int) -> spconv_batch:
         """The struct for a call on a cache of this many pages (a copy: the batch may serve several caches and threads)."""
-        s = spconv_batch.from_buffer_copy(self.struct)
-        s.pages = pages
-        return s
+        f = self._fields
+        return spconv_batch(f[0], f[1], f[2], f[3], f[4], pages, f[5], f[6], f[7], f[8])
 
 
 def _scaling(scaling):
@@ -222,7 +233,7 @@ def spconv_rope(x, positions, freq, interleaved: bool = False, inverse: bool = F
     pp = _whole(positions, "positions", torch.int32, (T,), device)
     fp, rot = _freq(freq, device)
     flags = (SPCONV_ROPE_INTERLEAVED if interleaved else 0) | (SPCONV_ROPE_INVERSE if inverse else 0)
-    with _On(device, stream) as raw:
+    with _on(device, stream) as raw:
         if out is None:
             out = torch.empty((T, H, D), dtype=x.dtype, device=device)
         op, ot, oh = _rows(out, "out", x.dtype, (T, H, D), device)
@@ -253,7 +264,7 @@ def spconv_cache_append(k, v, k_cache, v_cache, batch: CacheBatch, sums=None, fr
     pp = None if positions is None else _whole(positions, "positions", torch.int32, (T,), device)
     fp, rot = _freq(freq, device)
     flags = SPCONV_ROPE_INTERLEAVED if interleaved else 0
-    with _On(device, stream) as raw:
+    with _on(device, stream) as raw:
         _check(_lib.spconv_cache_append(code, batch.with_pages(pages), kp, kt, kh, vp, vt, vh, H, D, pp, fp, rot, flags,
                                         amplitude, kc, vc, sp, raw), "spconv_cache_append")
 
@@ -272,7 +283,7 @@ def spconv_block_scores(q, sums, batch: CacheBatch, out=None, stream=None):
     qp, qt, qh = _rows(q, "q", q.dtype, (T, HQ, D), device)
     sp = _whole(sums, "sums", torch.float32, (pages, H, D), device)
     shape = (batch.rows, H, batch.max_blocks)
-    with _On(device, stream) as raw:
+    with _on(device, stream) as raw:
         if out is None:
             out = torch.empty(shape, dtype=torch.float32, device=device)
         op = _whole(out, "out", torch.float32, shape, device)
@@ -290,7 +301,7 @@ def spconv_select_blocks(scores, batch: CacheBatch, keep: int, sink: int = 1, lo
         raise ValueError("scores must be [rows, heads, blocks]")
     H = scores.shape[1]
     sp = _whole(scores, "scores", torch.float32, (batch.rows, H, batch.max_blocks), device)
-    with _On(device, stream) as raw:
+    with _on(device, stream) as raw:
         if out is None:
             # Only sizes that the call accepts are allocated.
             if not 1 <= keep < 1 << 31:
@@ -303,12 +314,19 @@ def spconv_select_blocks(scores, batch: CacheBatch, keep: int, sink: int = 1, lo
     return out
 
 
+@lru_cache(maxsize=1024)
+def _workspace(code, sequences, block, max_blocks, q_block, tokens, one_each, q_heads, heads, dim, keep):
+    """Bytes of scratch memory: a function of these sizes alone (the batch's arrays are not looked at)."""
+    n = _i64()
+    batch = spconv_batch(sequences, block, max_blocks, q_block, tokens, 1, max_blocks, None, None, None if one_each else 16)
+    _check(_lib.spconv_attention_workspace(code, batch, q_heads, heads, dim, keep, n), "spconv_attention_workspace")
+    return n.value
+
+
 def spconv_attention_workspace(dtype, batch: CacheBatch, q_heads: int, heads: int, dim: int, keep: int = 0) -> int:
     """Bytes of scratch memory of a ``spconv_block_attention`` call of these sizes."""
-    n = _i64()
-    _check(_lib.spconv_attention_workspace(_DTYPES[dtype], batch.struct, q_heads, heads, dim, keep, n),
-           "spconv_attention_workspace")
-    return n.value
+    return _workspace(_DTYPES[dtype], batch.sequences, batch.block, batch.max_blocks, batch.q_block, batch.tokens,
+                      batch.q_start is None, q_heads, heads, dim, keep)
 
 
 def spconv_block_attention(q, k_cache, v_cache, batch: CacheBatch, blocks=None, counts=None, scale: float | None = None,
@@ -337,9 +355,9 @@ def spconv_block_attention(q, k_cache, v_cache, batch: CacheBatch, blocks=None, 
     if counts is not None:
         cp = _whole(counts, "counts", torch.int32, (batch.rows, H), device)
     struct = batch.with_pages(pages)
-    need = _i64()
-    _check(_lib.spconv_attention_workspace(code, struct, HQ, H, D, keep, need), "spconv_block_attention")
-    with _On(device, stream) as raw:
+    need = _workspace(code, batch.sequences, batch.block, batch.max_blocks, batch.q_block, batch.tokens,
+                      batch.q_start is None, HQ, H, D, keep)
+    with _on(device, stream) as raw:
         if out is None:
             out = torch.empty((T, HQ, D), dtype=q.dtype, device=device)
         op, ot, oh = _rows(out, "out", q.dtype, (T, HQ, D), device)
@@ -347,9 +365,9 @@ def spconv_block_attention(q, k_cache, v_cache, batch: CacheBatch, blocks=None, 
             lse = torch.empty((T, HQ), dtype=torch.float32, device=device)
         lp = None if lse is None or lse is False else _whole(lse, "lse", torch.float32, (T, HQ), device)
         wp, size = None, 0
-        if need.value:
+        if need:
             if workspace is None:
-                workspace = torch.empty(need.value, dtype=torch.uint8, device=device)
+                workspace = torch.empty(need, dtype=torch.uint8, device=device)
             if not isinstance(workspace, torch.Tensor) or workspace.device != device or not workspace.is_contiguous():
                 raise TypeError(f"workspace must be a contiguous tensor on {device}")
             wp, size = workspace.data_ptr(), workspace.numel() * workspace.element_size()

@@ -187,8 +187,8 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
         const int nv = (s1 - s0) * (int)a.vecs.d;
         for (int i = tid; i < nv; i += 256) {
             const int r = (uint32_t)i / a.vecs, c = (i - r * (int)a.vecs.d) * W;
-            *reinterpret_cast<V *>(vc + (int64_t)(s0 + r) * a.dim + c) =
-                *reinterpret_cast<const V *>((const T *)a.v + (int64_t)(s0 + r + t_off) * a.v_token + h * a.v_head + c);
+            const V x = *reinterpret_cast<const V *>((const T *)a.v + (int64_t)(s0 + r + t_off) * a.v_token + h * a.v_head + c);
+            __builtin_nontemporal_store(x, reinterpret_cast<V *>(vc + (int64_t)(s0 + r) * a.dim + c));
         }
         // Keys: rotated, stored, summed, older ones only summed; as many new rows at a time as the table holds.
         Floats<W> sum0, sum1;
@@ -282,8 +282,8 @@ int launch_append(AppendArgs &a, bool inter, hipStream_t stream) {
     a.rows = std::min(kTable / std::max(a.rot / 2, 1), a.B.q_start ? a.B.block : 1);
     a.table_len = a.rows * (a.rot / 2);
     const size_t lds = a.table_len * sizeof(CosSin) + (a.sums ? 256 / a.units.d * a.dim * sizeof(float) : 0);
-    // Heads a workgroup takes: as many as leave eight workgroups for every CU.
-    a.each = (int)std::min<int64_t>(std::max<int64_t>(a.items * a.heads / 2048, 1), a.heads);
+    // Heads a workgroup takes: as many as leave four workgroups for every CU.
+    a.each = (int)std::min<int64_t>(std::max<int64_t>(a.items * a.heads / 1024, 1), a.heads);
     a.head_groups = make_div((uint32_t)((a.heads + a.each - 1) / a.each));
     const dim3 grid = grid_of(a.items * a.head_groups.d);
     if (inter)
