@@ -78,7 +78,7 @@ struct AttnArgs {
     void *out;
     int64_t o_token, o_head;
     float *lse;
-    float *part, *stat;  // workspace, items from `whole` on: [item][split][tile_pairs][dim], [item][split][tile_pairs][2]
+    float *part, *stat;  // workspace, items from `whole` on: [item][split][tile_pairs][dim], [item][split][tile_pairs] of (maximum, sum, rounded sum, -)
     int64_t items;       // rows * heads * tiles
     int64_t whole;       // items [0, whole) are one workgroup each, those behind them `splits`
     int heads, group, dim, keep, tiles, splits, q_aligned, o_aligned;
@@ -459,8 +459,7 @@ __global__ __launch_bounds__(256) void rows_kernel(AttnArgs a) {
             const int64_t at = ((work.item - a.whole) * a.splits + work.split) * 16 + c;
             a.part[at * D + d] = acc;
             if (d == 0) {
-                a.stat[at * 2] = mx;
-                a.stat[at * 2 + 1] = l;
+                *reinterpret_cast<f32x4 *>(a.stat + at * 4) = f32x4{mx, l, l, 0.0f};
             }
         }
     }
@@ -488,6 +487,31 @@ __device__ __forceinline__ f32x16 mma32(frag_t<float> a, frag_t<float> b, f32x16
 __device__ __forceinline__ int fresh(int x) {
     asm volatile("" : "+v"(x));
     return x;
+}
+
+// Sum of the weights as they are rounded for the second product: the output is divided by it, so that the rounding of a
+// weight that outweighs all others cancels (the lazily raised maximum leaves it anywhere below 2^8). The log-sum-exp takes
+// the sum before rounding.
+template <typename T, int N>
+__device__ __forceinline__ float rounded_sum(const frag_t<T> (&w)[N]) {
+    float s[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) {
+            if constexpr (std::is_same<T, __bf16>::value) {
+                typedef __bf16 v2 __attribute__((ext_vector_type(2)));
+                s[(i >> 1) & 1] = __builtin_amdgcn_fdot2_f32_bf16(v2{w[n][i], w[n][i + 1]}, v2{(__bf16)1.0f, (__bf16)1.0f},
+                                                                  s[(i >> 1) & 1], false);
+            } else if constexpr (std::is_same<T, _Float16>::value) {
+                typedef _Float16 v2 __attribute__((ext_vector_type(2)));
+                s[(i >> 1) & 1] =
+                    __builtin_amdgcn_fdot2(v2{w[n][i], w[n][i + 1]}, v2{(_Float16)1.0f, (_Float16)1.0f}, s[(i >> 1) & 1], false);
+            } else {
+                s[(i >> 1) & 1] += w[n][i] + w[n][i + 1];
+            }
+        }
+    return s[0] + s[1];
 }
 
 // x, formed where this stands.
@@ -584,7 +608,7 @@ __global__ __launch_bounds__(THREADS, NK <= 4 && sizeof(T) == 2 ? 2 : 1) void ti
     for (int t = 0; t < NT; ++t)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[t][i] = 0.0f;
-    float top = -kInf, sum = 0.0f;  // top: of the products before scaling
+    float top = -kInf, sum = 0.0f, norm = 0.0f;  // top: of the products before scaling; norm: sum of the rounded weights
 
     constexpr bool two = THREADS == 512;  // two waves a SIMD
     const bool late = wave >= 4;
@@ -788,6 +812,7 @@ __global__ __launch_bounds__(THREADS, NK <= 4 && sizeof(T) == 2 ? 2 : 1) void ti
                 const float shrink = up == -kInf ? 1.0f : __builtin_amdgcn_exp2f((top - up) * scale2);
                 top = up;
                 sum *= shrink;
+                norm *= shrink;
 #pragma unroll
                 for (int n = 0; n < NT; ++n) o[n] *= shrink;
             }
@@ -812,8 +837,9 @@ __global__ __launch_bounds__(THREADS, NK <= 4 && sizeof(T) == 2 ? 2 : 1) void ti
                     total[i & 3] += x[b][i];
                     w[b * 2 + (i >> 3)][i & 7] = (T)x[b][i];
                 }
-            // (The sum is needed in the next tile only; formed there, it would keep all weights in registers.)
+            // (The sums are needed in the next tile only; formed there, they would keep all weights in registers.)
             sum = settled(sum + ((total[0] + total[1]) + (total[2] + total[3])));
+            norm = settled(norm + rounded_sum<T, NS>(w));
         };
 
         // Each tile takes a phase of matrix products (outputs of the tile before, products of this one) and
@@ -922,6 +948,7 @@ __global__ __launch_bounds__(THREADS, NK <= 4 && sizeof(T) == 2 ? 2 : 1) void ti
     const int out_tok = (uint32_t)out_m / a.group_div;
     const int64_t o_head_at = (int64_t)P.h * a.group + (out_m - out_tok * a.group);
     sum = half_sum(sum);
+    norm = half_sum(norm);
     const float ref = top == -kInf ? 0.0f : top * scale2;
     if (work.splits == 1) {
         T *dst = (T *)a.out + (int64_t)(P.r.t0 + out_tok) * a.o_token + o_head_at * a.o_head;
@@ -933,7 +960,7 @@ __global__ __launch_bounds__(THREADS, NK <= 4 && sizeof(T) == 2 ? 2 : 1) void ti
                 if (d >= D) continue;
                 V4 v;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = (T)weighted(o[t][i + e], sum);
+                for (int e = 0; e < 4; ++e) v[e] = (T)weighted(o[t][i + e], norm);
                 if (a.o_aligned) {
                     *reinterpret_cast<V4 *>(dst + d) = v;
                 } else {
@@ -953,8 +980,7 @@ __global__ __launch_bounds__(THREADS, NK <= 4 && sizeof(T) == 2 ? 2 : 1) void ti
                     *reinterpret_cast<f32x4 *>(a.part + at * D + d) = f32x4{o[t][i], o[t][i + 1], o[t][i + 2], o[t][i + 3]};
             }
         if (out_half == 0) {
-            a.stat[at * 2] = top == -kInf ? -kInf : top * scale2;
-            a.stat[at * 2 + 1] = sum;
+            *reinterpret_cast<f32x4 *>(a.stat + at * 4) = f32x4{top == -kInf ? -kInf : top * scale2, sum, norm, 0.0f};
         }
     }
 }
@@ -964,7 +990,7 @@ __global__ __launch_bounds__(THREADS, NK <= 4 && sizeof(T) == 2 ? 2 : 1) void ti
 template <typename T>
 __global__ __launch_bounds__(256) void join_kernel(AttnArgs a) {
     __shared__ float factor[512];
-    __shared__ float red[8];
+    __shared__ float red[12];
     __shared__ f32x4 sums[256];
     const int64_t idx = grid_index();
     if (idx >= (a.items - a.whole) * a.tile_pairs) return;
@@ -973,16 +999,17 @@ __global__ __launch_bounds__(256) void join_kernel(AttnArgs a) {
     const Pairs P = find_pairs(a, (uint32_t)a.whole + item);
     if (P.r.n == 0 || P.m0 + c >= P.end) return;
     const int step = a.tile_pairs;  // from share to share
-    const float *stat = a.stat + ((int64_t)item * a.splits * step + c) * 2;
+    const f32x4 *stat = reinterpret_cast<const f32x4 *>(a.stat) + ((int64_t)item * a.splits * step + c);
     const float *part = a.part + ((int64_t)item * a.splits * step + c) * a.dim;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    float x[2], y[2], mx = -kInf;
+    f32x4 x[2];
+    float mx = -kInf;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const int s = tid + i * 256;
-        x[i] = s < a.splits ? stat[s * step * 2] : -kInf;
-        y[i] = s < a.splits ? stat[s * step * 2 + 1] : 0.0f;
-        mx = fmaxf(mx, x[i]);
+        x[i] = f32x4{-kInf, 0.0f, 0.0f, 0.0f};
+        if (s < a.splits) x[i] = stat[s * step];
+        mx = fmaxf(mx, x[i][0]);
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
@@ -990,18 +1017,26 @@ __global__ __launch_bounds__(256) void join_kernel(AttnArgs a) {
     __syncthreads();
     mx = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
     const float ref = mx == -kInf ? 0.0f : mx;
-    float l = 0.0f;
+    float l = 0.0f, norm = 0.0f;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        const float f = __builtin_amdgcn_exp2f(x[i] - ref);
+        const float f = __builtin_amdgcn_exp2f(x[i][0] - ref);
         factor[tid + i * 256] = f;
-        l += f * y[i];
+        l += f * x[i][1];
+        norm += f * x[i][2];
     }
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) l += __shfl_xor(l, o);
-    if (lane == 0) red[4 + wave] = l;
+    for (int o = 32; o > 0; o >>= 1) {
+        l += __shfl_xor(l, o);
+        norm += __shfl_xor(norm, o);
+    }
+    if (lane == 0) {
+        red[4 + wave] = l;
+        red[8 + wave] = norm;
+    }
     __syncthreads();
     l = (red[4] + red[5]) + (red[6] + red[7]);
+    norm = (red[8] + red[9]) + (red[10] + red[11]);
 
     const int quads = a.dim / 4, groups = 256 / quads, g = tid / quads, u = tid - g * quads;
     f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -1018,7 +1053,7 @@ __global__ __launch_bounds__(256) void join_kernel(AttnArgs a) {
     const int m = P.m0 + c, tok = (uint32_t)m / a.group_div, head = P.h * a.group + (m - tok * a.group);
     T *dst = (T *)a.out + (int64_t)(P.r.t0 + tok) * a.o_token + (int64_t)head * a.o_head + u * 4;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) dst[e] = (T)weighted(acc[e], l);
+    for (int e = 0; e < 4; ++e) dst[e] = (T)weighted(acc[e], norm);
     if (a.lse && tid == 0) a.lse[(int64_t)(P.r.t0 + tok) * (a.heads * a.group) + head] = log_sum(ref, l);
 }
 
@@ -1056,7 +1091,7 @@ bool plan_of(int dtype, const spconv_batch *B, int q_heads, int heads, int dim, 
     p->part_bytes = p->bytes = 0;
     if (p->splits > 1) {
         p->part_bytes = rest * p->splits * p->tile_pairs * dim * 4;
-        p->bytes = p->part_bytes + rest * p->splits * p->tile_pairs * 2 * 4;
+        p->bytes = p->part_bytes + rest * p->splits * p->tile_pairs * 4 * 4;
     }
     return true;
 }
