@@ -513,9 +513,17 @@ __global__ __launch_bounds__(256) void select_wave_kernel(SelectArgs a) {
 }
 
 // One workgroup of 1024 threads a (row, head) of more blocks: wave w takes the w-th
-// sixteenth of them, in `per` steps of 64, from the cache each time (a count over all is one pass).
-__global__ __launch_bounds__(1024) void select_block_kernel(SelectArgs a, int per) {
+// sixteenth of them, in `per` steps of 64, the first kHeld of which (8192 blocks in all) stay in registers, the others
+// come from the cache each time. The want-th highest is found eight bits of its
+// order at a time, from the highest: how many of those that share the bits above have each of the 256 next ones is
+// counted in LDS (each number in eight places, so that lanes that count the same one wait less).
+// Two workgroups a CU, bound by the latency of its passes: 8192 blocks, 128 lists 12 us with the launch, 4096 lists
+// 101 us (134 MB); halving the order, 32 counts with a barrier each, took 54 and 426.
+__global__ __launch_bounds__(1024, 8) void select_block_kernel(SelectArgs a, int per) {
     __shared__ int counts[2][16];
+    __shared__ int bins[256][8];
+    __shared__ __attribute__((aligned(16))) int sums[256];
+    __shared__ int found[3];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t item = grid_index();
     if (item >= a.items) return;
@@ -531,68 +539,110 @@ __global__ __launch_bounds__(1024) void select_block_kernel(SelectArgs a, int pe
     }
     const float *s = a.scores + item * a.B.max_blocks;
     const int first = wave * per * 64;
+    const int steps = clamp_int((c.n - first + 63) / 64, 0, per);  // of this wave; behind them nothing is taken
     int turn = 0;
     // Sum over the workgroup of a wave's number, and of the waves before this one.
-    auto total = [&](int n, int &before) {
+    auto total = [&](int n, int &ahead) {
         if (lane == 0) counts[turn][wave] = n;
         __syncthreads();
         int all = 0;
-        before = 0;
+        ahead = 0;
         for (int w = 0; w < 16; ++w) {
-            if (w < wave) before += counts[turn][w];
+            if (w < wave) ahead += counts[turn][w];
             all += counts[turn][w];
         }
         turn ^= 1;  // the next one's slots: nobody is still reading those
         return all;
     };
-    auto value = [&](int j) { return j >= c.sink && j < c.low ? order_of(s[j]) : 0u; };
-    uint32_t cut = 0;
-    int above = -1, dummy;
+    constexpr int kHeld = 8;
+    float loaded[kHeld];
+    uint32_t held[kHeld];
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) loaded[i] = s[min(first + i * 64 + lane, c.n - 1)];
+    auto order = [&](int j, float x) { return j >= c.sink && j < c.low ? order_of(x) : 0u; };
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) held[i] = order(first + i * 64 + lane, loaded[i]);
+    // f(block, order of its value) for this wave's blocks.
+    auto each = [&](auto f) {
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i)
+            if (i < steps) f(first + i * 64 + lane, held[i]);
+#pragma unroll 4
+        for (int i = kHeld; i < steps; ++i) {
+            const int j = first + i * 64 + lane;
+            f(j, order(j, s[min(j, c.n - 1)]));
+        }
+    };
+    uint32_t cut = 0xffffffffu;  // what is above it is taken (no order is that high)
+    int ties = 0;                // and so many of those equal to it
     if (c.want > 0) {
-        for (int bit = 31; bit >= 0; --bit) {
-            const uint32_t t = cut | (1u << bit);
-            int n = 0;
-            for (int i = 0; i < per; ++i) n += bits(__ballot(value(first + i * 64 + lane) >= t));
-            n = total(n, dummy);
-            if (n >= c.want) {
-                cut = t;
-                above = n;
-                if (n == c.want) break;
+        int want = c.want, equal = 0;  // of those that share the bits found so far
+        cut = 0;
+        for (int shift = 24; shift >= 0; shift -= 8) {
+            for (int i = threadIdx.x; i < 256 * 8; i += 1024) bins[0][i] = 0;
+            __syncthreads();
+            each([&](int, uint32_t v) {
+                if (v != 0 && ((uint64_t)v >> (shift + 8)) == (uint64_t)cut >> (shift + 8))
+                    atomicAdd(&bins[(v >> shift) & 255][lane & 7], 1);
+            });
+            __syncthreads();
+            if (threadIdx.x < 256) {
+                int n = 0;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) n += bins[threadIdx.x][i];
+                sums[threadIdx.x] = n;
             }
+            __syncthreads();
+            if (wave == 0) {  // lane l: bins 4l .. 4l + 3
+                int n[4], mine = 0, above;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) mine += n[e] = sums[lane * 4 + e];
+                above = mine;  // with all lanes behind
+#pragma unroll
+                for (int o = 1; o < 64; o <<= 1) {
+                    const int x = __shfl_down(above, o);
+                    above += lane + o < 64 ? x : 0;
+                }
+                above -= mine;
+#pragma unroll
+                for (int e = 3; e >= 0; --e) {
+                    if (above < want && above + n[e] >= want) {  // one bin of one lane
+                        found[0] = lane * 4 + e;
+                        found[1] = above;
+                        found[2] = n[e];
+                    }
+                    above += n[e];
+                }
+            }
+            __syncthreads();
+            cut |= (uint32_t)found[0] << shift;
+            want -= found[1];
+            equal = found[2];
+            if (equal == want) break;  // all of them, whatever the bits below
         }
-    }
-    int ties = 0x7fffffff;
-    if (c.want <= 0) {
-        cut = 0xffffffffu;
-        ties = 0;
-    } else if (above != c.want) {
-        int n = 0, eq = 0, before;
-        for (int i = 0; i < per; ++i) {
-            const uint32_t v = value(first + i * 64 + lane);
-            n += bits(__ballot(v > cut));
-            eq += bits(__ballot(v == cut));
+        if (equal == want) {
+            cut = max(cut, 1u) - 1;  // (no candidate's order is 0)
+        } else {
+            int eq = 0, ahead;
+            each([&](int, uint32_t v) { eq += bits(__ballot(v == cut)); });
+            total(eq, ahead);
+            ties = max(0, want - ahead);
         }
-        n = total(n, dummy);
-        total(eq, before);
-        ties = max(0, c.want - n - before);
     }
     // Taken by this wave, then by those before it, then the list.
     int mine = 0, at = 0;
     for (int pass = 0; pass < 2; ++pass) {
         int left = ties, n = 0;
-        for (int i = 0; i < per; ++i) {
-            const int j = first + i * 64 + lane;
-            const uint32_t v = value(j);
-            const uint64_t below = (1ull << lane) - 1;
+        each([&](int j, uint32_t v) {
             const uint64_t eq = __ballot(v == cut);
-            const bool tie = v == cut && bits(eq & below) < left;
+            const bool tie = v == cut && before(eq) < left;
             const bool take = j < c.n && (j < c.sink || j >= c.low || v > cut || tie);
-            if (left != 0x7fffffff) left = max(0, left - bits(eq));
+            left = max(0, left - bits(eq));
             const uint64_t all = __ballot(take);
-            const int pos = at + n + bits(all & below);
+            const int pos = at + n + before(all);
             if (pass == 1 && take && pos < a.keep) blocks[pos] = j;
             n += bits(all);
-        }
+        });
         if (pass == 0) mine = total(n, at);
     }
     for (int i = mine + (int)threadIdx.x; i < a.keep; i += 1024) blocks[i] = -1;
@@ -646,6 +696,7 @@ extern "C" int spconv_select_blocks(const spconv_batch *batch, int heads, const 
     if (keep < always || items >= ((int64_t)1 << 31) || items * keep >= ((int64_t)1 << 40)) return SPCONV_EINVAL;
     SelectArgs a{*batch, scores, blocks, counts, items, heads, keep, sink, local, 1, make_div((uint32_t)heads)};
     const int n = (batch->max_blocks + 63) / 64;
+    // A wave's registers hold 2048 values: 4096 lists of 2048 blocks take 20 us, by workgroups 65 (128 lists: 12 and 10).
     if (n <= 32) {
         a.each = (int)std::min<int64_t>(std::max<int64_t>(items / 8192, 1), heads);  // 8192 waves fill the GPU
         const dim3 grid = grid_of(((items + a.each - 1) / a.each + 3) / 4);
