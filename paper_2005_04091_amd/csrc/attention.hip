@@ -206,8 +206,8 @@ __device__ __forceinline__ int row_unit(int r, int c) {
 // One workgroup a (row, head, 16 pairs, share of the row's keys). Its four waves take 32
 // keys in turn, each with a running maximum, sum and output of its own, joined
 // at the end; shares of a row (splits) are joined by join_kernel.
-template <typename T, int NK>
-__global__ __launch_bounds__(256) void rows_kernel(AttnArgs a) {
+template <typename T, int NK, int NC>
+__global__ __launch_bounds__(256, sizeof(T) == 2 && NC <= 4 ? 2 : 1) void rows_kernel(AttnArgs a) {
     constexpr int DP = NK * 32, W = kPer16<T>, UPR = DP / W;  // 16-byte units of a row
     constexpr int NU = 16 * UPR / 64;                         // units a lane holds of 16 rows
     constexpr int kTile = 32 * DP * (int)sizeof(T);
@@ -228,12 +228,12 @@ __global__ __launch_bounds__(256) void rows_kernel(AttnArgs a) {
     // Query of this lane's column.
     const int m = P.m0 + col, tok = (uint32_t)m / a.group_div;
     const int pos = tok < P.r.n ? P.r.p0 + tok : -1;
-    frag_t<T> q[NK];
+    frag_t<T> q[NC];
     {
         const T *src = (const T *)a.q + (int64_t)(P.r.t0 + tok) * a.q_token +
                        (int64_t)(P.h * a.group + (m - tok * a.group)) * a.q_head;
 #pragma unroll
-        for (int k = 0; k < NK; ++k) {
+        for (int k = 0; k < NC; ++k) {
             const int d = k * 32 + part * 8;
             q[k] = zero_frag<T>();
             if (tok < P.r.n && d < D) {
@@ -253,7 +253,7 @@ __global__ __launch_bounds__(256) void rows_kernel(AttnArgs a) {
     const int64_t s_lo = min(per * work.split, slabs), s_hi = min(s_lo + per, slabs);
     const int first_pos = P.r.p0 + (int)((uint32_t)P.m0 / a.group_div);  // position of the tile's first token
 
-    constexpr int NT = DP / 16;
+    constexpr int NT = NC * 2;
     f32x4 o[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) o[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -262,14 +262,14 @@ __global__ __launch_bounds__(256) void rows_kernel(AttnArgs a) {
 
     // Keys go from memory into the operands of the first product, values by rows through LDS, which hands
     // them out by columns. The next tile's loads start as soon as this one's registers are free.
-    frag_t<T> kf[2][NK];
+    frag_t<T> kf[2][NC];
     V vf[2][NU];
     auto fetch_keys = [&](int s) {
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             const T *src = (const T *)a.k_cache + S.base[s + t] + col * D;
 #pragma unroll
-            for (int k = 0; k < NK; ++k) {
+            for (int k = 0; k < NC; ++k) {
                 const int d = k * 32 + part * 8;
                 kf[t][k] = *reinterpret_cast<const frag_t<T> *>(src + (d < D ? d : 0));
             }
@@ -309,7 +309,7 @@ __global__ __launch_bounds__(256) void rows_kernel(AttnArgs a) {
             for (int t = 0; t < 2; ++t) {
                 x[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                for (int k = 0; k < NK; ++k) {
+                for (int k = 0; k < NC; ++k) {
                     frag_t<T> f = kf[t][k];
                     if (k * 32 + part * 8 >= D) f = zero_frag<T>();
                     x[t] = mma(f, q[k], x[t]);
@@ -375,7 +375,7 @@ __global__ __launch_bounds__(256) void rows_kernel(AttnArgs a) {
             __builtin_amdgcn_wave_barrier();
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
-                if (t * 16 >= D) break;
+                if (t * 16 >= D) continue;
                 frag_t<T> f;
                 if constexpr (sizeof(T) == 2) {
                     typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -410,14 +410,13 @@ __global__ __launch_bounds__(256) void rows_kernel(AttnArgs a) {
                         if (key0[t] + kr > pos) continue;
                         const T *src = (const T *)a.v_cache + S.base[s + t] + kr * D;
 #pragma unroll
-                        for (int n = 0; n < NT; ++n)
+                        for (int n = 0; n < NT; ++n) {
+                            const int d = n * 16 + part * 4;
+                            const Floats<4> v = load_floats<T, 4>(src + min(d, D - 4));
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                const int d = n * 16 + part * 4 + i;
-                                if (d >= D) continue;
-                                const float v = (float)src[d];
-                                if (not_finite(v)) o[n][i] += v;
-                            }
+                            for (int i = 0; i < 4; ++i) o[n][i] += not_finite(v.v[i]) ? v.v[i] : 0.0f;  // (behind D: not used)
+                            asm volatile("" ::: "memory");  // one load at a time: this is no place for registers
+                        }
                     }
                 }
             }
@@ -553,11 +552,11 @@ __device__ __forceinline__ int value_unit(int r, int c) {
 // The running maximum is raised only when a tile passes it by a factor of 2^8 or more: weights up
 // to 2^8 are as exact as those up to 1, and the output is rescaled a few times a row instead of
 // nearly every tile.
-template <typename T, int NK, int KT, int THREADS>
+template <typename T, int NK, int NC, int KT, int THREADS>
 __global__ __launch_bounds__(THREADS, NK <= 4 && sizeof(T) == 2 ? 2 : 1) void tiles_kernel(AttnArgs a) {
     constexpr int DP = NK * 32, W = kPer16<T>, UPR = DP / W, SIZE = (int)sizeof(T);
     constexpr int NL = KT * UPR / THREADS;  // units a thread stages of a tile's keys, and of its values
-    constexpr int NS = KT / 16, NB = KT / 32, NQ = DP / 16, NT = DP / 32;
+    constexpr int NS = KT / 16, NB = KT / 32, NQ = NC * 2, NT = NC;
     __shared__ __attribute__((aligned(16))) T lds[2][2][KT * DP];
     __shared__ Slabs S;
     __shared__ int any_odd;
@@ -657,7 +656,10 @@ __global__ __launch_bounds__(THREADS, NK <= 4 && sizeof(T) == 2 ? 2 : 1) void ti
         auto places = [&](int t) {
             Places p;
 #pragma unroll
-            for (int i = 0; i < NL; ++i) p.at[i] = S.base[t * NS + (i * THREADS + wave * 64) / UPR / 16];
+            for (int i = 0; i < NL; ++i) {
+                p.at[i] = S.base[t * NS + (i * THREADS + wave * 64) / UPR / 16];
+                if (NK == 8) p.at[i] = uniform64(p.at[i]);  // (the widest ones are short of vector registers)
+            }
             return p;
         };
         auto fetch = [&](V (&r)[NL], const void *cache, const Places &p) {
@@ -750,7 +752,7 @@ __global__ __launch_bounds__(THREADS, NK <= 4 && sizeof(T) == 2 ? 2 : 1) void ti
         // O^T += V^T P^T of tile t, if any, then S^T = K Q^T of tile t + 1. LDS reads run kLead matrix instructions
         // ahead of those that they feed.
         auto multiply = [&](auto with_outputs, int t) {
-            constexpr int kOut = decltype(with_outputs)::value ? NS * NT : 0, kAll = kOut + NQ * NB, kLead = 4;
+            constexpr int kOut = decltype(with_outputs)::value ? NS * NT : 0, kAll = kOut + NQ * NB, kLead = SIZE == 2 ? 4 : 2;
             const T *vs = lds[1][t & 1], *ks = lds[0][(t + 1) & 1];
             frag_t<T> f[kLead];
             auto read = [&](int i) {
@@ -772,6 +774,7 @@ __global__ __launch_bounds__(THREADS, NK <= 4 && sizeof(T) == 2 ? 2 : 1) void ti
                     x[b] = mma32(f[i % kLead], q[k], c);
                 }
                 if (i + kLead < kAll) f[i % kLead] = read(i + kLead);
+                if (SIZE == 4) __builtin_amdgcn_sched_barrier(0);
             }
             if constexpr (SIZE == 2) {
                 // (Without this the compiler puts each read right before its use.)
@@ -985,11 +988,13 @@ __global__ __launch_bounds__(THREADS, NK <= 4 && sizeof(T) == 2 ? 2 : 1) void ti
     }
 }
 
+constexpr int kMostSplits = 512;
+
 // Joins the shares of a pair: one workgroup a (row, head, tile, pair). The factors of the shares are formed by a
 // thread each, then the shares are summed by 256 / (dim / 4) groups of threads, four components a thread, eight loads ahead.
 template <typename T>
 __global__ __launch_bounds__(256) void join_kernel(AttnArgs a) {
-    __shared__ float factor[512];
+    __shared__ float factor[kMostSplits];
     __shared__ float red[12];
     __shared__ f32x4 sums[256];
     const int64_t idx = grid_index();
@@ -1002,6 +1007,7 @@ __global__ __launch_bounds__(256) void join_kernel(AttnArgs a) {
     const f32x4 *stat = reinterpret_cast<const f32x4 *>(a.stat) + ((int64_t)item * a.splits * step + c);
     const float *part = a.part + ((int64_t)item * a.splits * step + c) * a.dim;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    static_assert(kMostSplits == 2 * 256, "two shares a thread");
     f32x4 x[2];
     float mx = -kInf;
 #pragma unroll
@@ -1061,17 +1067,28 @@ struct Plan {
     int64_t items, whole;
     int waves;  // of the tiles kernel; 0: the rows kernel
     int tile_pairs, tiles, splits;
+    spconv_batch batch;  // with the rows of this call
     int64_t part_bytes, bytes;
 };
 
 // False for sizes out of range.
 bool plan_of(int dtype, const spconv_batch *B, int q_heads, int heads, int dim, int keep, Plan *p) {
     const int group = q_heads / heads;
+    const int most = dtype == SPCONV_F32 || dim > 128 ? 4 : 8;  // waves of a tile: registers of the wider ones
+    p->batch = *B;
+    // Without lists rows mean nothing to the result: they are as long as a tile has room for, and sequences tokens.
+    // (two sequences, 1000 tokens, 4 heads of 4 queries and 128 components, rows of one token given: 549 -> 94 us)
+    if (keep == 0 && B->q_start) {
+        const int64_t tokens = (B->tokens + B->sequences - 1) / B->sequences;
+        int q = std::min(std::max(most * 32 / group, 1), 128);
+        while (q > 1 && (q + 1) / 2 >= tokens) q = (q + 1) / 2;
+        p->batch.q_block = q;
+    }
+    B = &p->batch;
     const int64_t pairs = (int64_t)B->q_block * group;
     p->waves = 0;
     p->tile_pairs = 16;
     if (pairs > 16) {
-        const int most = dtype == SPCONV_F32 || dim > 128 ? 4 : 8;  // registers of the wider ones
         p->waves = 2;
         while (p->waves < most && p->waves * 32 < pairs) p->waves *= 2;
         p->tile_pairs = p->waves * 32;
@@ -1079,13 +1096,19 @@ bool plan_of(int dtype, const spconv_batch *B, int q_heads, int heads, int dim, 
     p->tiles = (int)((pairs + p->tile_pairs - 1) / p->tile_pairs);
     p->items = rows_of(B) * heads * p->tiles;
     if (p->items >= ((int64_t)1 << 27)) return false;
-    // The GPU holds `slots` workgroups at a time: one of eight waves on a CU, two of the smaller ones. Items that do not
+    // The GPU holds `slots` workgroups at a time: one of eight waves or of wide rows on a CU, two of the others. Items that do not
     // fill a round of them are split along their keys (128 keys a share at least), so that they do.
-    const int64_t slots = p->waves == 8 ? 256 : 512;
+    const int64_t slots = p->waves == 8 || (p->waves == 0 && dim > 128) ? 256 : 512;
     const int64_t keys = (int64_t)(keep ? keep : B->max_blocks) * B->block;
     const int64_t rest = p->items % slots;
     // (Behind sixteen full rounds the last one does not matter.)
-    const int64_t splits = rest && p->items <= 16 * slots ? std::min(slots / rest, (keys + 127) / 128) : 1;
+    // Without lists rows' keys differ, by sequence or by position: single tokens of several sequences, or tiles that would
+    // fill more than half a round, get two rounds of shares to even that out (48 sequences of 100 to 16384 keys, one head
+    // of 256 components: 99 -> 66 us; 4096 tokens, 16-bit, 192: 645 -> 368; of equal lengths, 16 sequences: 36 -> 41).
+    const bool uneven = keep == 0 && (p->waves == 0 ? B->sequences > 1 : rest > slots / 2);
+    const int64_t splits = rest && p->items <= 16 * slots
+                               ? std::min({(uneven ? 2 : 1) * slots / rest, (keys + 127) / 128, (int64_t)kMostSplits})
+                               : 1;
     p->splits = (int)std::max<int64_t>(1, splits);
     p->whole = p->splits > 1 ? p->items - rest : p->items;
     p->part_bytes = p->bytes = 0;
@@ -1096,14 +1119,14 @@ bool plan_of(int dtype, const spconv_batch *B, int q_heads, int heads, int dim, 
     return true;
 }
 
-template <typename T, int NK, int KT>
+template <typename T, int NK, int NC, int KT>
 void launch_tiles(const AttnArgs &a, int waves, dim3 grid, hipStream_t stream) {
     if (waves == 2)
-        tiles_kernel<T, NK, KT, 128><<<grid, 128, 0, stream>>>(a);
+        tiles_kernel<T, NK, NC, KT, 128><<<grid, 128, 0, stream>>>(a);
     else if (waves == 4)
-        tiles_kernel<T, NK, KT, 256><<<grid, 256, 0, stream>>>(a);
+        tiles_kernel<T, NK, NC, KT, 256><<<grid, 256, 0, stream>>>(a);
     else if constexpr (sizeof(T) == 2 && NK <= 4)
-        tiles_kernel<T, NK, KT, 512><<<grid, 512, 0, stream>>>(a);
+        tiles_kernel<T, NK, NC, KT, 512><<<grid, 512, 0, stream>>>(a);
 }
 
 template <typename T>
@@ -1111,18 +1134,22 @@ int attention_of(const AttnArgs &a, const Plan &p, hipStream_t stream) {
     const dim3 grid = grid_of(a.whole + (a.items - a.whole) * a.splits);
     if (p.waves == 0) {
         if (a.dim <= 64)
-            rows_kernel<T, 2><<<grid, 256, 0, stream>>>(a);
+            rows_kernel<T, 2, 2><<<grid, 256, 0, stream>>>(a);
         else if (a.dim <= 128)
-            rows_kernel<T, 4><<<grid, 256, 0, stream>>>(a);
+            rows_kernel<T, 4, 4><<<grid, 256, 0, stream>>>(a);
+        else if (a.dim <= 192)
+            rows_kernel<T, 8, 6><<<grid, 256, 0, stream>>>(a);
         else
-            rows_kernel<T, 8><<<grid, 256, 0, stream>>>(a);
+            rows_kernel<T, 8, 8><<<grid, 256, 0, stream>>>(a);
     } else {
         if (a.dim <= 64)
-            launch_tiles<T, 2, sizeof(T) == 4 ? 32 : 64>(a, p.waves, grid, stream);
+            launch_tiles<T, 2, 2, sizeof(T) == 4 ? 32 : 64>(a, p.waves, grid, stream);
         else if (a.dim <= 128)
-            launch_tiles<T, 4, sizeof(T) == 4 ? 32 : 64>(a, p.waves, grid, stream);
+            launch_tiles<T, 4, 4, sizeof(T) == 4 ? 32 : 64>(a, p.waves, grid, stream);
+        else if (a.dim <= 192)
+            launch_tiles<T, 8, 6, 32>(a, p.waves, grid, stream);
         else
-            launch_tiles<T, 8, 32>(a, p.waves, grid, stream);
+            launch_tiles<T, 8, 8, 32>(a, p.waves, grid, stream);
     }
     if (hipGetLastError() != hipSuccess) return SPCONV_EHIP;
     if (a.splits > 1) {
@@ -1157,10 +1184,13 @@ extern "C" int spconv_block_attention(int dtype, const spconv_batch *batch, cons
         (counts != nullptr && blocks == nullptr) || !plan_of(dtype, batch, q_heads, heads, dim, keep, &p))
         return SPCONV_EINVAL;
     if (p.bytes > 0 && (workspace == nullptr || !aligned16(workspace) || workspace_bytes < p.bytes)) return SPCONV_EINVAL;
-    AttnArgs a{*batch, q, q_token, q_head, k_cache, v_cache, blocks, counts, out, out_token, out_head, lse,
+    // Zero times what is masked, -infinity, would be NaN: the least number stands for a scale of zero (products
+    // below 2^100 come out as 0 all the same).
+    const float scale2 = scale == 0.0f ? 0x1p-149f : scale * kLog2e;
+    AttnArgs a{p.batch, q, q_token, q_head, k_cache, v_cache, blocks, counts, out, out_token, out_head, lse,
                (float *)workspace, nullptr, p.items, p.whole, heads, q_heads / heads, dim, keep, p.tiles, p.splits,
                rows_aligned16(q, q_token, q_head, size_of(dtype)),
-               rows_aligned16(out, out_token, out_head, size_of(dtype)), p.tile_pairs, scale * kLog2e,
+               rows_aligned16(out, out_token, out_head, size_of(dtype)), p.tile_pairs, scale2,
                make_div((uint32_t)p.tiles), make_div((uint32_t)heads), make_div((uint32_t)(q_heads / heads)),
                make_div((uint32_t)p.splits), make_div((uint32_t)(batch->block / 16)), make_div((uint32_t)p.tile_pairs)};
     if (p.bytes > 0) a.stat = (float *)((char *)workspace + p.part_bytes);

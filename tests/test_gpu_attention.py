@@ -331,6 +331,51 @@ def test_attention(dtype, case):
         check_attention(s, q, heads)
 
 
+WIDE = [
+    # lens, kv, block, heads, group, dim, q_block: wide heads in rows and in tiles of 64 and 128 pairs; lists longer than one
+    # look-up; more (row, head) items than the GPU holds at a time, with a rest that is split along its keys
+    ([5], [300], 32, 1, 2, 160, 1), ([20, 3], [150, 3], 16, 2, 4, 192, 8), ([70], [600], 64, 1, 4, 200, 33), ([40], [90], 16, 1, 8, 256, 16),
+    ([3, 9], [5000, 4500], 256, 1, 2, 32, 4), ([66], [4800], 128, 1, 4, 40, 64), ([530], [700], 16, 1, 2, 24, 1), ([4200], [4210], 256, 2, 2, 16, 16),
+    ([3], [4700], 64, 1, 1, 256, 1)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("case", WIDE, ids=str)
+def test_attention_wide_long_and_many(dtype, case):
+    lens, kv, block, heads, group, dim, q_block = case
+    rng = np.random.default_rng(sum(kv) * 3 + dim)
+    s = Setup(rng, lens, kv, block, heads, dim, dtype, q_block, extra_cols=1, tail=2)
+    q = normal(rng, (s.tokens, heads * group, dim), dtype)
+    check_attention(s, q, heads)
+    blocks, counts = random_lists(rng, s, heads, max(5, 4400 // block if kv[0] > 4400 else 5))
+    check_attention(s, q, heads, blocks, counts)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("q_block,group", [(1, 2), (8, 4), (64, 4)])
+def test_attention_of_a_scale_of_zero(dtype, q_block, group):
+    """Every seen key weighs the same, also where the keys are split and joined."""
+    rng = np.random.default_rng(q_block + 40)
+    s = Setup(rng, [9], [900], 16, 1, 64, dtype, q_block)
+    q = normal(rng, (s.tokens, group, 64), dtype)
+    blocks, counts = random_lists(rng, s, 1, 50)
+    check_attention(s, q, 1, blocks, counts, scale=0.0)
+    check_attention(s, q, 1, scale=0.0)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("dim,q_block", [(192, 1), (256, 1), (200, 16), (256, 16)])
+def test_attention_of_wide_values_that_are_not_finite(dtype, dim, q_block):
+    rng = np.random.default_rng(dim + q_block)
+    s = Setup(rng, [21], [90], 16, 1, dim, dtype, q_block)
+    q = normal(rng, (s.tokens, 4, dim), dtype)
+    for pos, d, x in [(80, 3, "inf"), (84, dim - 1, "nan"), (84, 5, "-inf"), (89, 7, "inf"), (10, 9, "inf"), (83, 100, "-inf"), (85, 100, "inf")]:
+        s.v[int(s.table[0, pos // 16]), 0, pos % 16, d] = float(x)
+    check_attention(s, q, 1)
+    blocks, counts = random_lists(rng, s, 1, 6)
+    check_attention(s, q, 1, blocks, counts)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("q_block,group", [(1, 4), (16, 2), (64, 4)])
 def test_attention_what_is_masked_takes_no_part(dtype, q_block, group):
