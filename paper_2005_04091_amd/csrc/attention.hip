@@ -50,6 +50,13 @@ __device__ __forceinline__ frag_t<T> zero_frag() {
     return z;
 }
 
+// x, as a value that the compiler knows nothing about: what is derived from it is formed where it
+// is used, and not kept in registers through the loops before.
+__device__ __forceinline__ int fresh(int x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
 // Max and sum over the four lanes that hold one column (lanes l, l+16, l+32, l+48).
 __device__ __forceinline__ float column_max(float x) {
     const uint32_t u = __float_as_uint(x);
@@ -213,6 +220,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && NC <= 4 ? 2 : 1) void rows_k
     constexpr int kTile = 32 * DP * (int)sizeof(T);
     constexpr int kJoin = 16 * (DP + 4) * 4;
     constexpr int kPerWave = kTile > kJoin ? kTile : kJoin;
+    // Addresses are formed anew for each tile where registers are short (fp32, 256 components: 128 -> 107 us; others lose 2%).
+    constexpr bool kFresh = NC == 8 && sizeof(T) == 4;
     __shared__ __attribute__((aligned(16))) char lds[4 * kPerWave];
     __shared__ Slabs S;
     __shared__ float w_max[4][16], w_sum[4][16];
@@ -279,9 +288,10 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && NC <= 4 ? 2 : 1) void rows_k
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             const T *src = (const T *)a.v_cache + S.base[s + t];
+            const int ln = kFresh ? fresh(lane) : lane;
 #pragma unroll
             for (int i = 0; i < NU; ++i) {
-                const int u = i * 64 + lane, c = u % UPR;
+                const int u = i * 64 + ln, c = u % UPR;
                 vf[t][i] = *reinterpret_cast<const V *>(src + u / UPR * D + (c * W < D ? c * W : 0));
             }
         }
@@ -335,11 +345,12 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && NC <= 4 ? 2 : 1) void rows_k
                         }
                     }
             }
+            const int ln = kFresh ? fresh(lane) : lane;
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int i = 0; i < NU; ++i) {
-                    const int u = i * 64 + lane, r = t * 16 + u / UPR;
+                    const int u = i * 64 + ln, r = t * 16 + u / UPR;
                     *reinterpret_cast<V *>(vt + r * DP + row_unit<UPR, (int)sizeof(T)>(r, u % UPR) * W) = vf[t][i];
                 }
             if (s + 8 < n_slabs) fetch_values(s + 8);
@@ -386,7 +397,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && NC <= 4 ? 2 : 1) void rows_k
                     } u;
 #pragma unroll
                     for (int b = 0; b < 2; ++b) {
-                        const int lr = b * 16 + part * 4 + (col >> 2);
+                        const int col = ln & 15, part = ln >> 4, lr = b * 16 + part * 4 + (col >> 2);
                         const int c = t * 2 + ((col & 3) >> 1);
                         T *src = vt + lr * DP + row_unit<UPR, 2>(lr, c) * W + (col & 1) * 4;
                         u.h[b] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)src);
@@ -395,7 +406,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && NC <= 4 ? 2 : 1) void rows_k
                 } else {
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        const int lr = (i >> 2) * 16 + part * 4 + (i & 3), d = t * 16 + col;
+                        const int lr = (i >> 2) * 16 + (ln >> 4) * 4 + (i & 3), d = t * 16 + (ln & 15);
                         f[i] = vt[lr * DP + row_unit<UPR, 4>(lr, d >> 2) * 4 + (d & 3)];
                     }
                 }
@@ -479,13 +490,6 @@ __device__ __forceinline__ f32x16 mma32(frag_t<float> a, frag_t<float> b, f32x16
 #pragma unroll
     for (int i = 0; i < 8; ++i) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[i], b[i], c, 0, 0, 0);
     return c;
-}
-
-// x, as a value that the compiler knows nothing about: what is derived from it is formed where it
-// is used, and not kept in registers through the loops before.
-__device__ __forceinline__ int fresh(int x) {
-    asm volatile("" : "+v"(x));
-    return x;
 }
 
 // Sum of the weights as they are rounded for the second product: the output is divided by it, so that the rounding of a
@@ -1089,7 +1093,7 @@ bool plan_of(int dtype, const spconv_batch *B, int q_heads, int heads, int dim, 
     p->waves = 0;
     p->tile_pairs = 16;
     if (pairs > 16) {
-        p->waves = 2;
+        p->waves = dim > 192 ? 4 : 2;  // (the widest ones' registers hold a quarter of a tile's loads, not a half)
         while (p->waves < most && p->waves * 32 < pairs) p->waves *= 2;
         p->tile_pairs = p->waves * 32;
     }
@@ -1121,12 +1125,13 @@ bool plan_of(int dtype, const spconv_batch *B, int q_heads, int heads, int dim, 
 
 template <typename T, int NK, int NC, int KT>
 void launch_tiles(const AttnArgs &a, int waves, dim3 grid, hipStream_t stream) {
-    if (waves == 2)
-        tiles_kernel<T, NK, NC, KT, 128><<<grid, 128, 0, stream>>>(a);
-    else if (waves == 4)
+    if (waves == 4) {
         tiles_kernel<T, NK, NC, KT, 256><<<grid, 256, 0, stream>>>(a);
-    else if constexpr (sizeof(T) == 2 && NK <= 4)
-        tiles_kernel<T, NK, NC, KT, 512><<<grid, 512, 0, stream>>>(a);
+    } else if (waves == 2) {
+        if constexpr (NC <= 6) tiles_kernel<T, NK, NC, KT, 128><<<grid, 128, 0, stream>>>(a);
+    } else {
+        if constexpr (sizeof(T) == 2 && NK <= 4) tiles_kernel<T, NK, NC, KT, 512><<<grid, 512, 0, stream>>>(a);
+    }
 }
 
 template <typename T>
