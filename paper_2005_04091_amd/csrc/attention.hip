@@ -1092,7 +1092,11 @@ bool plan_of(int dtype, const spconv_batch *B, int q_heads, int heads, int dim, 
     const int64_t pairs = (int64_t)B->q_block * group;
     p->waves = 0;
     p->tile_pairs = 16;
-    if (pairs > 16) {
+    // Rows of more pairs than these are tiles of 32 pairs for each of some waves. (Wide ones keep a CU busy with four waves
+    // only, of which few pairs leave three or two idle: 32 pairs of 2000 tokens, 256 components, 239 us by tiles and 210 by
+    // rows; fp32 1134 and 567, 64 pairs 712 and 562.)
+    const int few = dim <= 128 ? 16 : dtype == SPCONV_F32 ? 64 : dim > 192 ? 32 : 16;
+    if (pairs > few) {
         p->waves = dim > 192 ? 4 : 2;  // (the widest ones' registers hold a quarter of a tile's loads, not a half)
         while (p->waves < most && p->waves * 32 < pairs) p->waves *= 2;
         p->tile_pairs = p->waves * 32;
@@ -1128,7 +1132,7 @@ void launch_tiles(const AttnArgs &a, int waves, dim3 grid, hipStream_t stream) {
     if (waves == 4) {
         tiles_kernel<T, NK, NC, KT, 256><<<grid, 256, 0, stream>>>(a);
     } else if (waves == 2) {
-        if constexpr (NC <= 6) tiles_kernel<T, NK, NC, KT, 128><<<grid, 128, 0, stream>>>(a);
+        if constexpr (NC <= (sizeof(T) == 2 ? 6 : 4)) tiles_kernel<T, NK, NC, KT, 128><<<grid, 128, 0, stream>>>(a);
     } else {
         if constexpr (sizeof(T) == 2 && NK <= 4) tiles_kernel<T, NK, NC, KT, 512><<<grid, 512, 0, stream>>>(a);
     }
