@@ -191,10 +191,11 @@ inline bool heads_ok(int q_heads, int heads, int dim) {
 
 inline bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
 
-// Whether rows of these strides (elements) can be read by 16-byte vectors.
-inline bool rows_aligned16(const void *p, int64_t a, int64_t b, int size) {
-    return aligned16(p) && a * size % 16 == 0 && b * size % 16 == 0;
+// Whether rows of these strides (elements of `size` bytes) can be read by vectors of w elements, a power of two.
+inline bool rows_aligned(const void *p, int64_t a, int64_t b, int size, int w) {
+    return ((uintptr_t)p & (uintptr_t)(size * w - 1)) == 0 && a % w == 0 && b % w == 0;
 }
+inline bool rows_aligned16(const void *p, int64_t a, int64_t b, int size) { return rows_aligned(p, a, b, size, 16 / size); }
 
 // Strides of a tensor that is written: no two rows of dim elements overlap along one axis.
 inline bool out_strides_ok(int64_t tokens, int heads, int dim, int64_t token, int64_t head) {

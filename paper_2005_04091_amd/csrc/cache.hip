@@ -68,7 +68,10 @@ struct RopeArgs {
 };
 
 // A workgroup takes `group` tokens: their sines and cosines into LDS, once for all
-// heads, then every (token, head, vector pair) by one thread.
+// heads, then every (token, head, vector pair) by one thread. Vectors are the widest that pairs and copies split into.
+// 16384 tokens, 32 heads, bf16: 128 components in whole vectors 44 us, 6.1 TB/s (of inputs that the last-level cache
+// does not hold 50 us, 5.4); rot 40 of 96 by four components 4.4 TB/s, rot 36 of 80 by two 4.0, rot 26 of
+// 88, one by one, 2.2, bound by the number of its loads and stores.
 template <typename T, int W, bool INTER>
 __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
     extern __shared__ CosSin table[];
@@ -86,28 +89,42 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
         }
         __syncthreads();
         const int total = n * (int)a.row.d;
-        for (int i = tid; i < total; i += 256) {
-            const int t = (uint32_t)i / a.row, r = i - t * (int)a.row.d;
-            const int h = (uint32_t)r / a.units, u = r - h * (int)a.units.d;
-            const T *xr = x + (t0 + t) * a.x_token + h * a.x_head;
-            T *yr = out + (t0 + t) * a.o_token + h * a.o_head;
-            if (u * W < a.rot / 2) {
-                int d0, d1;
-                pair_at<W, INTER>(u, a.rot, d0, d1);
-                Floats<W> p = load_floats<T, W>(xr + d0), q = load_floats<T, W>(xr + d1);
-                CosSin m[W];
+        // Narrow vectors: as many on their way as make 16 bytes, four at most.
+        constexpr int kAhead = 16 / (W * (int)sizeof(T)) < 4 ? 16 / (W * (int)sizeof(T)) : 4;
+        for (int i0 = tid; i0 < total; i0 += 256 * kAhead) {
+            typedef typename VecOf<T, W>::type V;
+            V p[kAhead], q[kAhead];
+            T *y0[kAhead], *y1[kAhead];
+            const CosSin *angles[kAhead];  // null: copied
 #pragma unroll
-                for (int k = 0; k < W; ++k) m[k] = table[t * (int)a.half.d + u * W + k];
-                rotate<W, INTER>(p, q, m);
-                store_floats<T, W>(yr + d0, p);
-                store_floats<T, W>(yr + d1, q);
-            } else {
-                const int d = a.rot / 2 + u * W;  // rot + (u - rot/2/W) * W
-                if constexpr (W == 1) {
-                    yr[d] = xr[d];
+            for (int k = 0; k < kAhead; ++k) {
+                const int i = min(i0 + 256 * k, total - 1);
+                const int t = (uint32_t)i / a.row, r = i - t * (int)a.row.d;
+                const int h = (uint32_t)r / a.units, u = r - h * (int)a.units.d;
+                const T *xr = x + (t0 + t) * a.x_token + h * a.x_head;
+                T *yr = out + (t0 + t) * a.o_token + h * a.o_head;
+                int d0 = a.rot / 2 + u * W, d1 = d0;  // copied: rot + (u - rot/2/W) * W
+                const bool pair = u * W < a.rot / 2;
+                if (pair) pair_at<W, INTER>(u, a.rot, d0, d1);
+                angles[k] = pair ? table + t * (int)a.half.d + u * W : nullptr;
+                p[k] = *reinterpret_cast<const V *>(xr + d0);
+                q[k] = *reinterpret_cast<const V *>(xr + d1);
+                y0[k] = yr + d0;
+                y1[k] = yr + d1;
+            }
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                if (kAhead > 1 && i0 + 256 * k >= total) break;
+                if (angles[k]) {
+                    Floats<W> f = floats_of<T, W>(p[k]), g = floats_of<T, W>(q[k]);
+                    CosSin m[W];
+#pragma unroll
+                    for (int e = 0; e < W; ++e) m[e] = angles[k][e];
+                    rotate<W, INTER>(f, g, m);
+                    store_floats<T, W>(y0[k], f);
+                    store_floats<T, W>(y1[k], g);
                 } else {
-                    typedef typename VecOf<T, W>::type V;
-                    *reinterpret_cast<V *>(yr + d) = *reinterpret_cast<const V *>(xr + d);
+                    *reinterpret_cast<V *>(y0[k]) = p[k];
                 }
             }
         }
@@ -256,10 +273,12 @@ int launch_rope(const RopeArgs &a, bool inter, int blocks, size_t lds, hipStream
 
 template <typename T>
 int rope_of(RopeArgs &a, bool inter, hipStream_t stream) {
-    constexpr int V = kPer16<T>;
-    const bool vec = splits_into(a.dim, a.rot, V) && rows_aligned16(a.x, a.x_token, a.x_head, sizeof(T)) &&
-                     rows_aligned16(a.out, a.o_token, a.o_head, sizeof(T));
-    const int units = (a.dim - a.rot / 2) / (vec ? V : 1);
+    // The widest vectors that pairs and copies split into and that rows are aligned for.
+    int w = kPer16<T>;
+    while (w > 1 && !(splits_into(a.dim, a.rot, w) && rows_aligned(a.x, a.x_token, a.x_head, sizeof(T), w) &&
+                      rows_aligned(a.out, a.o_token, a.o_head, sizeof(T), w)))
+        w /= 2;
+    const int units = (a.dim - a.rot / 2) / w;
     a.units = make_div((uint32_t)units);
     a.row = make_div((uint32_t)units * (uint32_t)a.heads);
     // Tokens a workgroup takes at a time: about 1024 vector pairs, sines within 32 KiB, and
@@ -271,7 +290,12 @@ int rope_of(RopeArgs &a, bool inter, hipStream_t stream) {
     const int64_t groups = (a.tokens + group - 1) / group;
     const int blocks = (int)std::min<int64_t>(groups, 1 << 20);
     const size_t lds = (size_t)group * (a.rot / 2) * sizeof(CosSin);
-    return vec ? launch_rope<T, V>(a, inter, blocks, lds, stream) : launch_rope<T, 1>(a, inter, blocks, lds, stream);
+    if (w == 8) {
+        if constexpr (kPer16<T> == 8) return launch_rope<T, 8>(a, inter, blocks, lds, stream);
+    }
+    if (w == 4) return launch_rope<T, 4>(a, inter, blocks, lds, stream);
+    if (w == 2) return launch_rope<T, 2>(a, inter, blocks, lds, stream);
+    return launch_rope<T, 1>(a, inter, blocks, lds, stream);
 }
 
 template <typename T, int W>
