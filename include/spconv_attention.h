@@ -142,11 +142,11 @@ int spconv_rope(int dtype, const void *x, int64_t x_token, int64_t x_head, int64
  * read may be shared); the slots of two sequences in one page are otherwise stored in an unspecified order.
  * k, v       device, [tokens][heads][dim] by strides as in spconv_rope.
  * k_cache, v_cache  device [pages][heads][block][dim], 16-byte aligned.
- * sums       device fp32 [pages][heads][dim], 16-byte aligned, nullable.
+ * sums       device fp32 [pages][heads][dim], 16-byte aligned, nullable. None of the outputs may overlap the inputs.
  * positions  device int32 [tokens], nullable.  freq  device fp64 [rot/2], nullable (no rotation; rot must be 0).
  * flags, amplitude  as spconv_rope, without SPCONV_ROPE_INVERSE.
  * heads      1 to 65535.   dim  a multiple of 8, 8 to 256.   batch->q_block is not used.
- * Errors: SPCONV_EINVAL as above; SPCONV_EHIP when the launch fails.
+ * Errors: SPCONV_EINVAL as above, and for (tokens/block + 2*sequences)*heads >= 2^31; SPCONV_EHIP when the launch fails.
  */
 int spconv_cache_append(int dtype, const spconv_batch *batch, const void *k, int64_t k_token, int64_t k_head,
                         const void *v, int64_t v_token, int64_t v_head, int heads, int dim, const int32_t *positions,
@@ -162,9 +162,10 @@ int spconv_cache_append(int dtype, const spconv_batch *batch, const void *k, int
  * token of the row sees, blocks without a page and rows without tokens get -infinity.
  * q        device, [tokens][q_heads][dim] by strides; query head g belongs to key head g / (q_heads/heads).
  * sums     device fp32 [pages][heads][dim], 16-byte aligned, as spconv_cache_append keeps them.
- * scores   device fp32 [R][heads][max_blocks]; every element is written.
+ * scores   device fp32 [R][heads][max_blocks]; every element is written, must not overlap the inputs.
  * Errors: SPCONV_EINVAL (NULL pointer, bad batch, unknown dtype, q_heads not a multiple of heads or
- * above 65535, dim not a multiple of 8 in [8, 256], R*heads >= 2^31, a negative stride); SPCONV_EHIP.
+ * above 65535, dim not a multiple of 8 in [8, 256], R*heads*ceil(max_blocks/64) >= 2^31, a negative stride);
+ * SPCONV_EHIP.
  */
 int spconv_block_scores(int dtype, const spconv_batch *batch, const void *q, int64_t q_token, int64_t q_head,
                         int q_heads, int heads, int dim, const float *sums, float *scores, hipStream_t stream);
@@ -202,7 +203,7 @@ int spconv_attention_workspace(int dtype, const spconv_batch *batch, int q_heads
  * Keys that a token does not see take no part whatever they hold (infinities and NaN among it).
  * blocks   device int32 [R][heads][keep], any order; entries outside [0, max_blocks) and blocks without a page
  *          are passed over, a block that is listed twice counts twice. NULL (with keep 0 and counts NULL): every
- *          visible block.
+ *          visible block (what batch->q_block says is then of no matter).
  * counts   device int32 [R][heads], nullable (then all keep entries are looked at); taken into [0, keep].
  * k_cache, v_cache  device [pages][heads][block][dim], 16-byte aligned.
  * out      device, [tokens][q_heads][dim] by strides, must not overlap the inputs.
@@ -213,8 +214,8 @@ int spconv_attention_workspace(int dtype, const spconv_batch *batch, int q_heads
  * Results are reproducible run to run for a given device and sizes.
  * Errors: SPCONV_EINVAL (NULL pointer, bad batch, unknown dtype, q_heads not a multiple of heads or above 65535,
  * dim not a multiple of 8 in [8, 256], a negative stride, a scale that is not finite, keep < 0, blocks without keep or keep without
- * blocks, counts without blocks, R*heads*ceil(q_block*q_heads/heads/16) >= 2^27, a workspace that is too small or
- * misaligned); SPCONV_EHIP.
+ * blocks, counts without blocks, out == q, 2^27 tiles or more of 16 to 256 (token, head) pairs of a row, a workspace
+ * that is too small or misaligned); SPCONV_EHIP.
  */
 int spconv_block_attention(int dtype, const spconv_batch *batch, const void *q, int64_t q_token, int64_t q_head,
                            int q_heads, int heads, int dim, const void *k_cache, const void *v_cache, float scale,

@@ -138,6 +138,8 @@ def _elsewhere(device, stream):
         if stream is None:
             yield torch.cuda.current_stream(device).cuda_stream
         else:
+            if stream.device != device:
+                raise ValueError(f"stream belongs to {stream.device}, the tensors to {device}")
             with torch.cuda.stream(stream):
                 yield stream.cuda_stream
 

@@ -94,9 +94,9 @@ inline dim3 grid_of(int64_t n) {
 __device__ __forceinline__ int64_t grid_index() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
 
 // The last sequence b whose start, q_start[b]/div + mul*b, is at most x (the same for the whole wave, as is
-// the result), found by the whole wave, 64 sequences a step, and its tokens. The starts do not decrease; where
-// they do (the array is the caller's) some sequence or none comes out, with
-// its tokens taken into the batch.
+// the result), found by the whole wave, 64 starts a step, each step between two of the last one's, and its
+// tokens. The starts do not decrease; where they do (the array is the caller's) some sequence or none comes
+// out, with its tokens taken into the batch.
 struct Seq {
     int b;          // -1: none
     int first, n;   // tokens [first, first + n)
@@ -119,19 +119,24 @@ __device__ __forceinline__ Seq find_seq(const spconv_batch &B, int x, int div, i
         s.at = 0;
     } else {
         const int lane = threadIdx.x & (kWave - 1);
-        int count = 0;
-        for (int b0 = 0; b0 < B.sequences; b0 += kWave) {
-            const int b = b0 + lane;
+        s.b = 0;
+        for (int left = B.sequences, step; left > 0; left = step > 1 ? min(step, left) : 0) {  // among [s.b, s.b + left)
+            step = (left + kWave - 1) / kWave;
+            const int64_t i = (int64_t)lane * step;
             bool in = false;
-            if (b < B.sequences)
+            if (i < left) {
+                const int b = s.b + (int)i;
                 in = (int64_t)(clamp_int(B.q_start[b], 0, tokens) / div) + (int64_t)mul * b <= (int64_t)x;
-            const int c = __popcll(__ballot(in));
-            count += c;
-            if (c < kWave) break;
+            }
+            const int last = (int)__popcll(__ballot(in)) - 1;
+            if (last < 0) {  // (before the first start; behind the first step the first of them is one)
+                s.b = -1;
+                s.first = s.n = s.at = s.kv = 0;
+                return s;
+            }
+            s.b += last * step;
+            left -= last * step;
         }
-        s.b = count - 1;
-        s.first = s.n = s.at = s.kv = 0;
-        if (s.b < 0) return s;
         s.first = clamp_int(uniform(B.q_start[s.b]), 0, tokens);
         s.n = max(clamp_int(uniform(B.q_start[s.b + 1]), 0, tokens) - s.first, 0);
         s.at = (int)((int64_t)x - (s.first / div) - (int64_t)mul * s.b);

@@ -575,6 +575,131 @@ def test_a_step_in_a_graph():
         assert all(torch.equal(a, b) for a, b in zip((layer.k_cache, layer.v_cache, layer.sums), after)), i
 
 
+@pytest.mark.parametrize("B,q_block", [(70, 1), (70, 4), (5000, 1), (5000, 8)])
+def test_many_short_sequences(B, q_block):
+    """Rows are found among more sequences than a wave compares at a time, empty ones among them."""
+    rng = np.random.default_rng(B + q_block)
+    lens = rng.integers(0, 3, B) if B > 100 else rng.integers(0, 12, B)
+    s = Setup(rng, lens, lens + rng.integers(0, 20, B), 16, 1, 16, torch.bfloat16, q_block, tail=1)
+    q = normal(rng, (s.tokens, 2, 16), torch.bfloat16)
+    check_attention(s, q, 1)
+    blocks, counts = random_lists(rng, s, 1, 3)
+    check_attention(s, q, 1, blocks, counts)
+    sums = torch.randn((s.pages, 1, 16), device=DEV)
+    want, bound = O.scores(s.rows, f64(q), f64(sums), s.table, s.kv, 16, 1)
+    got = A.spconv_block_scores(q, sums, s.batch)
+    near(got, want, bound)
+    wb, wc = O.select(s.rows, got.cpu().numpy(), 16, 2, 0, 1)
+    blocks, counts = A.spconv_select_blocks(got, s.batch, 2, 0, 1)
+    assert np.array_equal(blocks.cpu().numpy(), wb) and np.array_equal(counts.cpu().numpy(), wc)
+    # Keys of every sequence end up at the end of its pages.
+    k, v = (normal(rng, (s.tokens, 1, 16), torch.bfloat16) for _ in range(2))
+    kc, vc = s.k.clone(), s.v.clone()
+    A.spconv_cache_append(k, v, kc, vc, s.batch)
+    for b in range(0, B, 1 if B < 100 else 37):
+        for i in range(lens[b]):
+            at = s.kv[b] - lens[b] + i
+            page = int(s.table[b, at // 16])
+            assert torch.equal(kc[page, 0, at % 16], k[s.start[b] + i, 0]) and torch.equal(vc[page, 0, at % 16], v[s.start[b] + i, 0])
+
+
+def test_sequences_that_share_their_first_pages():
+    rng = np.random.default_rng(51)
+    for q_block, lens in ((1, [3, 2, 5]), (8, [20, 9, 33])):
+        s = Setup(rng, lens, [200, 180, 222], 16, 2, 64, torch.float16, q_block)
+        s.table[1, :9] = s.table[2, :9] = s.table[0, :9]
+        s.make()
+        q = normal(rng, (s.tokens, 6, 64), torch.float16)
+        k, v = (normal(rng, (s.tokens, 2, 64), torch.float16) for _ in range(2))
+        sums = torch.randn((s.pages, 2, 64), device=DEV)
+        before = sums.clone()
+        A.spconv_cache_append(k, v, s.k, s.v, s.batch, sums)
+        shared = torch.from_numpy(s.table[0, :9].astype(np.int64)).to(DEV)
+        assert torch.equal(sums[shared], before[shared])  # only read
+        want, bound = O.scores(s.rows, f64(q), f64(sums), s.table, s.kv, 16, 2)
+        scores = A.spconv_block_scores(q, sums, s.batch)
+        near(scores, want, bound)
+        blocks, counts = A.spconv_select_blocks(scores, s.batch, 8, 1, 2)
+        check_attention(s, q, 2, blocks.cpu().numpy(), counts.cpu().numpy())
+        check_attention(s, q, 2)
+
+
+@pytest.mark.parametrize("keep,q_block", [(6, 16), (0, 16), (5, 1)])
+def test_prompts_in_a_graph(keep, q_block):
+    """A captured step of ragged prompts, replayed after others of other lengths in the same buffers."""
+    rng = np.random.default_rng(keep + q_block)
+    heads, dim, block, B, T = 2, 64, 16, 3, 90
+    layer = A.BlockAttention(130, heads, dim, block, keep, 1, 2, dtype=torch.float16, device=DEV)
+    layer.k_cache.normal_()
+    layer.v_cache.normal_()
+    if keep:
+        layer.sums.normal_()
+    state = [t.clone() for t in (layer.k_cache, layer.v_cache, layer.sums) if t is not None]
+    table = torch.from_numpy(rng.permutation(130)[:120].reshape(B, 40).astype(np.int32)).to(DEV)
+    kv = torch.zeros(B, dtype=torch.int32, device=DEV)
+    start = torch.zeros(B + 1, dtype=torch.int32, device=DEV)
+    pos = torch.zeros(T, dtype=torch.int32, device=DEV)
+    q = torch.zeros((T, 4, dim), dtype=torch.float16, device=DEV)
+    k, v = (torch.zeros((T, heads, dim), dtype=torch.float16, device=DEV) for _ in range(2))
+    batch = A.CacheBatch(table, kv, block, start, T, q_block)
+    out, lse = torch.zeros_like(q), torch.zeros((T, 4), device=DEV)
+
+    def load(i):
+        r = np.random.default_rng(200 + i)
+        for t in (q, k, v):
+            t.copy_(normal(r, tuple(t.shape), torch.float16))
+        cut = np.sort(r.integers(0, T + 1, B + 1)).astype(np.int32)
+        lens = np.diff(cut)
+        keys = (lens + r.integers(0, 640 - T, B)).astype(np.int32)
+        start.copy_(torch.from_numpy(cut))
+        kv.copy_(torch.from_numpy(keys))
+        p = np.zeros(T, np.int32)
+        for b in range(B):
+            p[cut[b]:cut[b + 1]] = np.arange(keys[b] - lens[b], keys[b])
+        pos.copy_(torch.from_numpy(p))
+
+    def fresh():
+        for t, c in zip([t for t in (layer.k_cache, layer.v_cache, layer.sums) if t is not None], state):
+            t.copy_(c)
+        out.fill_(5.0)
+        lse.fill_(5.0)
+
+    load(0)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        layer.step(q, k, v, pos, batch, out, lse)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        layer.step(q, k, v, pos, batch, out, lse)
+    for i in range(4):
+        load(i)
+        fresh()
+        layer.step(q, k, v, pos, batch, out, lse)
+        eager = [out.clone(), lse.clone(), layer.k_cache.clone()]
+        fresh()
+        torch.cuda.synchronize()
+        graph.replay()
+        assert all(torch.equal(a, b) for a, b in zip((out, lse, layer.k_cache), eager)), i
+
+
+def test_a_stream_of_another_device_is_refused():
+    class Elsewhere:
+        device, cuda_stream = torch.device("cuda", 7), 0
+
+    x = torch.zeros((1, 1, 8), device=DEV)
+    with pytest.raises(ValueError):
+        A.spconv_rope(x, torch.zeros(1, dtype=torch.int32, device=DEV), torch.ones(2, dtype=torch.float64, device=DEV), stream=Elsewhere())
+
+
+def test_queries_as_outputs_are_refused():
+    s = Setup(np.random.default_rng(1), [1], [20], 16, 1, 8, torch.float32, decode=True)
+    q = torch.zeros((1, 1, 8), device=DEV)
+    with pytest.raises(A.SpconvError):
+        A.spconv_block_attention(q, s.k, s.v, s.batch, out=q)
+
+
 def test_two_streams_at_once():
     """Two steps on two streams with workspaces of their own give their serial results."""
     rng = np.random.default_rng(33)
