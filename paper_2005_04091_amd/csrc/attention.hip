@@ -212,7 +212,12 @@ __device__ __forceinline__ int row_unit(int r, int c) {
 
 // One workgroup a (row, head, 16 pairs, share of the row's keys). Its four waves take 32
 // keys in turn, each with a running maximum, sum and output of its own, joined
-// at the end; shares of a row (splits) are joined by join_kernel.
+// at the end; shares of a row (splits) are joined by join_kernel. NK*32 components are laid out, NC*32 computed.
+// The keys are read once for 16 pairs, so single tokens are bound by HBM: 64 tokens, 8 heads of 4 queries, 128
+// components, bf16, lists of 2048 keys, 97 us, 5.5 TB/s. Two workgroups a CU (one of more than 128 components, whose
+// tiles fill the registers): 16 tokens, 4 heads of 8 queries, 256 components, 42 us, 3.2 TB/s; fp32 108 us, 2.5 TB/s,
+// some of it in scratch memory. Lists of prompts that come from the caches: 1000 rows of one token, 4 heads of 4
+// queries, 512 keys, 117 us, 9 TB/s.
 template <typename T, int NK, int NC>
 __global__ __launch_bounds__(256, sizeof(T) == 2 && NC <= 4 ? 2 : 1) void rows_kernel(AttnArgs a) {
     constexpr int DP = NK * 32, W = kPer16<T>, UPR = DP / W;  // 16-byte units of a row
@@ -551,8 +556,12 @@ __device__ __forceinline__ int value_unit(int r, int c) {
 // One workgroup a (row, head, 32 pairs for each of its waves, share of the row's keys): the waves
 // walk the keys together, KT at a time, staged in LDS, each with the queries, the
 // statistics and the output of its own 32 pairs in registers.
-// While a tile is computed the next one is on its way to registers; it is put into the other
-// half of the LDS behind the computation, one barrier a tile.
+// While a tile is computed the next one is on its way to registers; from there it is put into the other
+// half of the LDS. Bound by the matrix unit and, at four waves or less, by what those wait for. 8192 tokens in rows of
+// 64, 8 heads of 4 queries, 128 components, bf16, lists of 2048 keys: 349 us, 760 TFLOP/s of the products that count
+// (no masked ones) with eight waves a workgroup, 367 us with four. Wide ones have no room for eight: 4096
+// tokens of 2 sequences, 4 queries a head, 192 components 365 TFLOP/s, 256 components 273. fp32 runs at half of
+// its matrix unit's rate (128 components, 78 TFLOP/s), 256 components, in part in scratch memory, at 33.
 // The running maximum is raised only when a tile passes it by a factor of 2^8 or more: weights up
 // to 2^8 are as exact as those up to 1, and the output is rescaled a few times a row instead of
 // nearly every tile.
@@ -994,7 +1003,8 @@ __global__ __launch_bounds__(THREADS, NK <= 4 && sizeof(T) == 2 ? 2 : 1) void ti
 
 constexpr int kMostSplits = 512;
 
-// Joins the shares of a pair: one workgroup a (row, head, tile, pair). The factors of the shares are formed by a
+// Joins the shares of a pair (64 shares of 32 pairs of 128 components 4.5 us, the latency of two dependent loads and
+// the launch): one workgroup a (row, head, tile, pair). The factors of the shares are formed by a
 // thread each, then the shares are summed by 256 / (dim / 4) groups of threads, four components a thread, eight loads ahead.
 template <typename T>
 __global__ __launch_bounds__(256) void join_kernel(AttnArgs a) {
@@ -1078,7 +1088,7 @@ struct Plan {
 // False for sizes out of range.
 bool plan_of(int dtype, const spconv_batch *B, int q_heads, int heads, int dim, int keep, Plan *p) {
     const int group = q_heads / heads;
-    const int most = dtype == SPCONV_F32 || dim > 128 ? 4 : 8;  // waves of a tile: registers of the wider ones
+    const int most = dtype == SPCONV_F32 || dim > 128 ? 4 : 8;  // waves of a tile: two a SIMD where registers allow
     p->batch = *B;
     // Without lists rows mean nothing to the result: they are as long as a tile has room for, and sequences tokens.
     // (two sequences, 1000 tokens, 4 heads of 4 queries and 128 components, rows of one token given: 549 -> 94 us)
@@ -1092,10 +1102,12 @@ bool plan_of(int dtype, const spconv_batch *B, int q_heads, int heads, int dim, 
     const int64_t pairs = (int64_t)B->q_block * group;
     p->waves = 0;
     p->tile_pairs = 16;
-    // Rows of more pairs than these are tiles of 32 pairs for each of some waves. (Wide ones keep a CU busy with four waves
+    // Rows of more pairs than these are tiles of 32 pairs for each of some waves. (128 components, bf16, 2000 tokens: 16
+    // pairs 73 us by rows and 123 by tiles, 32 pairs 74 and 64; fp32 of 64 components, 32 pairs: 86 and 107. Wide ones keep a CU busy with four waves
     // only, of which few pairs leave three or two idle: 32 pairs of 2000 tokens, 256 components, 239 us by tiles and 210 by
     // rows; fp32 1134 and 567, 64 pairs 712 and 562.)
-    const int few = dim <= 128 ? 16 : dtype == SPCONV_F32 ? 64 : dim > 192 ? 32 : 16;
+    const bool f32 = dtype == SPCONV_F32;
+    const int few = dim <= 64 ? (f32 ? 32 : 16) : dim <= 128 ? 16 : f32 ? 64 : dim > 192 ? 32 : 16;
     if (pairs > few) {
         p->waves = dim > 192 ? 4 : 2;  // (the widest ones' registers hold a quarter of a tile's loads, not a half)
         while (p->waves < most && p->waves * 32 < pairs) p->waves *= 2;
@@ -1106,7 +1118,7 @@ bool plan_of(int dtype, const spconv_batch *B, int q_heads, int heads, int dim, 
     if (p->items >= ((int64_t)1 << 27)) return false;
     // The GPU holds `slots` workgroups at a time: one of eight waves or of wide rows on a CU, two of the others. Items that do not
     // fill a round of them are split along their keys (128 keys a share at least), so that they do.
-    const int64_t slots = p->waves == 8 || (p->waves == 0 && dim > 128) ? 256 : 512;
+    const int64_t slots = p->waves == 8 || (p->waves == 0 && dim > (f32 ? 64 : 128)) ? 256 : 512;
     const int64_t keys = (int64_t)(keep ? keep : B->max_blocks) * B->block;
     const int64_t rest = p->items % slots;
     // (Behind sixteen full rounds the last one does not matter.)
