@@ -7,7 +7,8 @@
 // Angles: position * frequency in turns is formed in fp64 and taken to the nearest
 // whole turn there (positions up to 2^31 turn the fastest pair 3e8 times: fp32 would
 // lose the fraction), then the rest, at most half a turn, goes through fp32 sine and
-// cosine of a multiple of pi, a relative error of 2^-24 or so whatever the position.
+// cosine of a multiple of pi, and what its rounding to fp32 left out comes in by their derivatives: an
+// error of 2^-24 or so whatever the position.
 #include "batch.h"
 
 namespace {
@@ -18,10 +19,11 @@ struct CosSin {
 
 __device__ __forceinline__ CosSin rope_angle(int position, double freq, float sign, float amplitude) {
     const double turns = (double)position * (freq * 0.15915494309189533577);  // 1 / (2 pi)
-    const float half_turns = (float)((turns - rint(turns)) * 2.0);
+    const double half_turns = (turns - rint(turns)) * 2.0;
+    const float near = (float)half_turns, rest = (float)(half_turns - near) * 3.14159265f;  // sin(a + r) = sin a + r cos a
     float s, c;
-    sincospif(half_turns, &s, &c);
-    return {c * amplitude, s * amplitude * sign};
+    sincospif(near, &s, &c);
+    return {fmaf(-s, rest, c) * amplitude, fmaf(c, rest, s) * amplitude * sign};
 }
 
 // W pairs: x of the first components, y of the second ones (half layout), or, in
