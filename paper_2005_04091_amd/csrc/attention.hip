@@ -1001,9 +1001,9 @@ __global__ __launch_bounds__(THREADS, NK <= 4 && sizeof(T) == 2 ? 2 : 1) void ti
     }
 }
 
-constexpr int kMostSplits = 512;
+constexpr int kMostSplits = 512, kFewSplits = 16;
 
-// Joins the shares of a pair (64 shares of 32 pairs of 128 components 4.5 us, the latency of two dependent loads and
+// Joins many shares of a pair (64 shares of 32 pairs of 128 components 4.5 us, the latency of two dependent loads and
 // the launch): one workgroup a (row, head, tile, pair). The factors of the shares are formed by a
 // thread each, then the shares are summed by 256 / (dim / 4) groups of threads, four components a thread, eight loads ahead.
 template <typename T>
@@ -1077,6 +1077,43 @@ __global__ __launch_bounds__(256) void join_kernel(AttnArgs a) {
     if (a.lse && tid == 0) a.lse[(int64_t)(P.r.t0 + tok) * (a.heads * a.group) + head] = log_sum(ref, l);
 }
 
+// The same for few shares: `lanes` (a power of two, 16 to 64, dim / 4 or more) threads a pair, four components each, over
+// all shares; a workgroup's pairs are of one tile. (A workgroup a pair spends its time on being started: 248 tiles of 128
+// pairs, two shares of 64 components, whole call 75 us by that and 30 by this; 42 shares of 16 tiles 23 and 32.)
+template <typename T>
+__global__ __launch_bounds__(256) void join_few_kernel(AttnArgs a, int lanes_log2) {
+    const int pairs = 256 >> lanes_log2;  // of a workgroup
+    const int64_t idx = grid_index() * pairs;
+    if (idx >= (a.items - a.whole) * a.tile_pairs) return;
+    const uint32_t item = (uint32_t)idx / a.pair_div;  // from `whole` on
+    const int c = (int)((uint32_t)idx - item * a.pair_div.d) + (int)(threadIdx.x >> lanes_log2);
+    const Pairs P = find_pairs(a, (uint32_t)a.whole + item);
+    const int u = threadIdx.x & ((1 << lanes_log2) - 1);
+    if (P.r.n == 0 || P.m0 + c >= P.end || u * 4 >= a.dim) return;
+    const int step = a.tile_pairs;  // from share to share
+    const f32x4 *stat = reinterpret_cast<const f32x4 *>(a.stat) + ((int64_t)item * a.splits * step + c);
+    const float *part = a.part + ((int64_t)item * a.splits * step + c) * a.dim + u * 4;
+    float mx = -kInf;
+#pragma unroll 4
+    for (int s = 0; s < a.splits; ++s) mx = fmaxf(mx, stat[s * step][0]);
+    const float ref = mx == -kInf ? 0.0f : mx;
+    float l = 0.0f, norm = 0.0f;
+    f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+    for (int s = 0; s < a.splits; ++s) {
+        const f32x4 x = stat[s * step];
+        const float f = __builtin_amdgcn_exp2f(x[0] - ref);
+        l += f * x[1];
+        norm += f * x[2];
+        acc += f * *reinterpret_cast<const f32x4 *>(part + (int64_t)s * step * a.dim);
+    }
+    const int m = P.m0 + c, tok = (uint32_t)m / a.group_div, head = P.h * a.group + (m - tok * a.group);
+    T *dst = (T *)a.out + (int64_t)(P.r.t0 + tok) * a.o_token + (int64_t)head * a.o_head + u * 4;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) dst[e] = (T)weighted(acc[e], norm);
+    if (a.lse && u == 0) a.lse[(int64_t)(P.r.t0 + tok) * (a.heads * a.group) + head] = log_sum(ref, l);
+}
+
 struct Plan {
     int64_t items, whole;
     int waves;  // of the tiles kernel; 0: the rows kernel
@@ -1108,7 +1145,9 @@ bool plan_of(int dtype, const spconv_batch *B, int q_heads, int heads, int dim, 
     // rows; fp32 1134 and 567, 64 pairs 712 and 562.)
     const bool f32 = dtype == SPCONV_F32;
     const int few = dim <= 64 ? (f32 ? 32 : 16) : dim <= 128 ? 16 : f32 ? 64 : dim > 192 ? 32 : 16;
-    if (pairs > few) {
+    // (fp32 of more than 192: five and a half tiles of 16 pairs cost one of 128; 132 pairs 615 and 737 us.)
+    const bool by_rows = pairs <= few || (f32 && dim > 192 && (pairs + 15) / 16 * 2 < (pairs + 127) / 128 * 11);
+    if (!by_rows) {
         p->waves = dim > 192 ? 4 : 2;  // (the widest ones' registers hold a quarter of a tile's loads, not a half)
         while (p->waves < most && p->waves * 32 < pairs) p->waves *= 2;
         p->tile_pairs = p->waves * 32;
@@ -1174,7 +1213,14 @@ int attention_of(const AttnArgs &a, const Plan &p, hipStream_t stream) {
     }
     if (hipGetLastError() != hipSuccess) return SPCONV_EHIP;
     if (a.splits > 1) {
-        join_kernel<T><<<grid_of((a.items - a.whole) * a.tile_pairs), 256, 0, stream>>>(a);
+        const int64_t pairs = (a.items - a.whole) * a.tile_pairs;
+        if (a.splits <= kFewSplits) {
+            const int lanes_log2 = a.dim <= 64 ? 4 : a.dim <= 128 ? 5 : 6;
+            const int64_t per = 256 >> lanes_log2;
+            join_few_kernel<T><<<grid_of((pairs + per - 1) / per), 256, 0, stream>>>(a, lanes_log2);
+        } else {
+            join_kernel<T><<<grid_of(pairs), 256, 0, stream>>>(a);
+        }
         return launched();
     }
     return SPCONV_OK;
