@@ -1140,9 +1140,9 @@ bool plan_of(int dtype, const spconv_batch *B, int q_heads, int heads, int dim, 
     p->waves = 0;
     p->tile_pairs = 16;
     // Rows of more pairs than these are tiles of 32 pairs for each of some waves. (128 components, bf16, 2000 tokens: 16
-    // pairs 73 us by rows and 123 by tiles, 32 pairs 74 and 64; fp32 of 64 components, 32 pairs: 86 and 107. Wide ones keep a CU busy with four waves
-    // only, of which few pairs leave three or two idle: 32 pairs of 2000 tokens, 256 components, 239 us by tiles and 210 by
-    // rows; fp32 1134 and 567, 64 pairs 712 and 562.)
+    // pairs 73 us by rows and 123 by tiles, 32 pairs 74 and 64; fp32 of 64 components, 32 pairs: 86 and 107. Wide ones
+    // keep a CU busy with four waves only, of which few pairs leave three or two idle: 32 pairs of 2000 tokens, 256
+    // components, 239 us by tiles and 210 by rows; fp32 1134 and 567, 64 pairs 712 and 562.)
     const bool f32 = dtype == SPCONV_F32;
     const int few = dim <= 64 ? (f32 ? 32 : 16) : dim <= 128 ? 16 : f32 ? 64 : dim > 192 ? 32 : 16;
     // (fp32 of more than 192: five and a half tiles of 16 pairs cost one of 128; 132 pairs 615 and 737 us.)
@@ -1155,8 +1155,8 @@ bool plan_of(int dtype, const spconv_batch *B, int q_heads, int heads, int dim, 
     p->tiles = (int)((pairs + p->tile_pairs - 1) / p->tile_pairs);
     p->items = rows_of(B) * heads * p->tiles;
     if (p->items >= ((int64_t)1 << 27)) return false;
-    // The GPU holds `slots` workgroups at a time: one of eight waves or of wide rows on a CU, two of the others. Items that do not
-    // fill a round of them are split along their keys (128 keys a share at least), so that they do.
+    // The GPU holds `slots` workgroups at a time: one of eight waves or of wide rows on a CU, two of the others. Items that
+    // do not fill a round of them are split along their keys (128 keys a share at least), so that they do.
     const int64_t slots = p->waves == 8 || (p->waves == 0 && dim > (f32 ? 64 : 128)) ? 256 : 512;
     const int64_t keys = (int64_t)(keep ? keep : B->max_blocks) * B->block;
     const int64_t rest = p->items % slots;
@@ -1165,7 +1165,10 @@ bool plan_of(int dtype, const spconv_batch *B, int q_heads, int heads, int dim, 
     // fill more than half a round, get two rounds of shares to even that out (48 sequences of 100 to 16384 keys, one head
     // of 256 components: 99 -> 66 us; 4096 tokens, 16-bit, 192: 645 -> 368; of equal lengths, 16 sequences: 36 -> 41).
     const bool uneven = keep == 0 && (p->waves == 0 ? B->sequences > 1 : rest > slots / 2);
-    const int64_t splits = rest && p->items <= 16 * slots
+    // Few keys are walked sooner than a second launch comes (8 lists of 512 keys of 128 components, bf16: 19 us, split 24;
+    // fp32 28 and 23).
+    const bool short_rows = p->waves == 0 ? keys * dim * size_of(dtype) <= 128 << 10 : keys <= 256;
+    const int64_t splits = rest && !short_rows && p->items <= 16 * slots
                                ? std::min({(uneven ? 2 : 1) * slots / rest, (keys + 127) / 128, (int64_t)kMostSplits})
                                : 1;
     p->splits = (int)std::max<int64_t>(1, splits);
