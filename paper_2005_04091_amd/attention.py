@@ -153,6 +153,15 @@ def _on(device, stream):
     return _elsewhere(device, stream)
 
 
+@lru_cache(maxsize=1024)
+def _batch_rows(sequences, block, max_blocks, q_block, tokens, stride, one_each):
+    """Rows of a batch, and its checks: a function of these sizes alone (the batch's arrays are not looked at)."""
+    rows = _i64()
+    batch = spconv_batch(sequences, block, max_blocks, q_block, tokens, 1, stride, None, None, None if one_each else 16)
+    _check(_lib.spconv_batch_rows(batch, rows), "spconv_batch_rows")
+    return rows.value
+
+
 class CacheBatch:
     """The sequences of a step (``struct spconv_batch``): ``table`` int32 [sequences, blocks] (pages), ``kv_len``
     int32 [sequences] (keys, the new ones among them), ``block`` keys to a page, ``q_start`` int32 [sequences + 1] (the
@@ -176,15 +185,16 @@ class CacheBatch:
         self.sequences, self.max_blocks, self.block, self.q_block, self.tokens = B, nb, block, q_block, tokens
         self._fields = (B, block, nb, q_block, tokens, stride, table.data_ptr(), kv_len.data_ptr(),
                         None if q_start is None else q_start.data_ptr())
-        self.struct = self.with_pages(1)  # until a call knows the cache
-        rows = _i64()
-        _check(_lib.spconv_batch_rows(self.struct, rows), "spconv_batch_rows")
-        self.rows = rows.value
+        self.rows = _batch_rows(B, block, nb, q_block, tokens, stride, q_start is None)
+        self._last = (0, None)
 
     def with_pages(self, pages: int) -> spconv_batch:
-        """The struct for a call on a cache of this many pages (a copy: the batch may serve several caches and threads)."""
-        f = self._fields
-        return spconv_batch(f[0], f[1], f[2], f[3], f[4], pages, f[5], f[6], f[7], f[8])
+        """The struct for a call on a cache of this many pages (never changed: calls and threads may share it)."""
+        last = self._last
+        if last[0] != pages:
+            f = self._fields
+            self._last = last = (pages, spconv_batch(f[0], f[1], f[2], f[3], f[4], pages, f[5], f[6], f[7], f[8]))
+        return last[1]
 
 
 def _scaling(scaling):
@@ -237,7 +247,7 @@ def spconv_rope(x, positions, freq, interleaved: bool = False, inverse: bool = F
     flags = (SPCONV_ROPE_INTERLEAVED if interleaved else 0) | (SPCONV_ROPE_INVERSE if inverse else 0)
     with _on(device, stream) as raw:
         if out is None:
-            out = torch.empty((T, H, D), dtype=x.dtype, device=device)
+            out = x.new_empty((T, H, D))
         op, ot, oh = _rows(out, "out", x.dtype, (T, H, D), device)
         _check(_lib.spconv_rope(code, xp, xt, xh, T, H, D, pp, fp, rot, flags, amplitude, op, ot, oh, raw), "spconv_rope")
     return out
@@ -287,7 +297,7 @@ def spconv_block_scores(q, sums, batch: CacheBatch, out=None, stream=None):
     shape = (batch.rows, H, batch.max_blocks)
     with _on(device, stream) as raw:
         if out is None:
-            out = torch.empty(shape, dtype=torch.float32, device=device)
+            out = sums.new_empty(shape)
         op = _whole(out, "out", torch.float32, shape, device)
         _check(_lib.spconv_block_scores(code, batch.with_pages(pages), qp, qt, qh, HQ, H, D, sp, op, raw),
                "spconv_block_scores")
@@ -308,8 +318,8 @@ def spconv_select_blocks(scores, batch: CacheBatch, keep: int, sink: int = 1, lo
             # Only sizes that the call accepts are allocated.
             if not 1 <= keep < 1 << 31:
                 raise SpconvError(SPCONV_EINVAL, "spconv_select_blocks")
-            out = (torch.empty((batch.rows, H, keep), dtype=torch.int32, device=device),
-                   torch.empty((batch.rows, H), dtype=torch.int32, device=device))
+            out = (scores.new_empty((batch.rows, H, keep), dtype=torch.int32),
+                   scores.new_empty((batch.rows, H), dtype=torch.int32))
         bp = _whole(out[0], "blocks", torch.int32, (batch.rows, H, keep), device)
         cp = _whole(out[1], "counts", torch.int32, (batch.rows, H), device)
         _check(_lib.spconv_select_blocks(batch.with_pages(1), H, sp, keep, sink, local, bp, cp, raw), "spconv_select_blocks")
@@ -361,15 +371,15 @@ def spconv_block_attention(q, k_cache, v_cache, batch: CacheBatch, blocks=None, 
                       batch.q_start is None, HQ, H, D, keep)
     with _on(device, stream) as raw:
         if out is None:
-            out = torch.empty((T, HQ, D), dtype=q.dtype, device=device)
+            out = q.new_empty((T, HQ, D))
         op, ot, oh = _rows(out, "out", q.dtype, (T, HQ, D), device)
         if lse is True:
-            lse = torch.empty((T, HQ), dtype=torch.float32, device=device)
+            lse = q.new_empty((T, HQ), dtype=torch.float32)
         lp = None if lse is None or lse is False else _whole(lse, "lse", torch.float32, (T, HQ), device)
         wp, size = None, 0
         if need:
             if workspace is None:
-                workspace = torch.empty(need, dtype=torch.uint8, device=device)
+                workspace = q.new_empty(need, dtype=torch.uint8)
             if not isinstance(workspace, torch.Tensor) or workspace.device != device or not workspace.is_contiguous():
                 raise TypeError(f"workspace must be a contiguous tensor on {device}")
             wp, size = workspace.data_ptr(), workspace.numel() * workspace.element_size()
