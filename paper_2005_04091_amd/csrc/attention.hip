@@ -99,6 +99,7 @@ struct Pairs {
     Row r;
     int h, m0, end;   // pairs [m0, end)
     int last;         // position of the tile's last token, -1 if it has none
+    int listed;       // what counts says of the row's list
     int64_t rh;
 };
 
@@ -109,6 +110,7 @@ __device__ __forceinline__ Pairs find_pairs(const AttnArgs &a, uint32_t item) {
     const int row = (int)(rh / a.head_div);
     p.h = (int)(rh - row * a.head_div.d);
     p.rh = rh;
+    p.listed = a.counts ? a.counts[rh] : a.keep;  // (on its way while the row is looked up)
     p.r = find_row(a.B, row);
     p.end = min(p.r.n * a.group, p.m0 + a.tile_pairs);
     p.last = p.end > p.m0 ? p.r.p0 + (int)((uint32_t)(p.end - 1) / a.group_div) : -1;
@@ -191,7 +193,7 @@ __device__ __forceinline__ int64_t slabs_of(const AttnArgs &a, const Pairs &P) {
     int entries = 0;
     if (P.last >= 0)
         entries = !a.blocks ? min(P.last / a.B.block + 1, a.B.max_blocks)
-                            : a.counts ? clamp_int(a.counts[P.rh], 0, a.keep) : a.keep;
+                            : clamp_int(P.listed, 0, a.keep);
     return (int64_t)entries * (a.B.block >> 4);
 }
 
