@@ -146,13 +146,16 @@ struct AppendArgs {
     int each;       // heads that a workgroup takes one after another
     int rows;       // rows of a page whose sines fit the table at a time
     int table_len;
-    Div head_groups, half, units, vecs;  // heads / each; rot/2; vectors of a key (pairs and copies); vectors of a value
+    int all_units, all_vecs;             // vectors of a key (pairs and copies) and of a value
+    Div parts, head_groups;              // workgroups that share a page's components; heads / each
+    Div units, vecs, half;               // of a part: vectors of a key and of a value, pairs
     float amplitude;
 };
 
 constexpr int kTable = 4096;  // sines and cosines in LDS at most
 
-// One workgroup a (touched page, group of heads). The pages that sequence b touches are items
+// One workgroup a (touched page, group of heads, part of the components: one part where there are enough pages and heads
+// for the GPU; 2254 tokens of 4 sequences, one head of 192, pages of 128 keys: 26 us by one part, 15 by three). The pages that sequence b touches are items
 // q_start[b]/block + 2b and on: a sequence of n tokens touches n/block + 2 pages at
 // most. Sines and cosines of the page's new tokens are formed once for the group's heads, in LDS. Threads hold one
 // vector pair of a key each and walk the page's rows in strides, so that the
@@ -165,9 +168,11 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
     float *part = reinterpret_cast<float *>(table + a.table_len);  // [groups][dim] partial sums
     typedef typename VecOf<T, W>::type V;
     const int64_t idx = grid_index();
-    if (idx >= a.items * a.head_groups.d) return;
-    const uint32_t item = (uint32_t)idx / a.head_groups;
-    const int h0 = (int)((uint32_t)idx - item * a.head_groups.d) * a.each;
+    if (idx >= a.items * a.head_groups.d * a.parts.d) return;
+    const uint32_t whole = (uint32_t)idx / a.parts;
+    const int share = (int)((uint32_t)idx - whole * a.parts.d);
+    const uint32_t item = whole / a.head_groups;
+    const int h0 = (int)(whole - item * a.head_groups.d) * a.each;
     const spconv_batch &B = a.B;
     const Seq s = find_seq(B, (int)item, B.block, 2);
     if (s.b < 0 || s.at < 0 || s.n == 0 || s.kv == 0) return;
@@ -182,19 +187,24 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
     const int tid = threadIdx.x;
 
     const int units = a.units.d, groups = 256 / units;
-    const int g = (uint32_t)tid / a.units, u = tid - g * units;
+    const int g = (uint32_t)tid / a.units, ul = tid - g * units, u0 = share * units, u = u0 + ul;
+    const bool mine = g < groups && u < a.all_units;
     const bool pair = u * W < a.rot / 2;
-    int d0, d1 = 0;
-    if (pair)
-        pair_at<W, INTER>(u, a.rot, d0, d1);
-    else
-        d0 = a.rot / 2 + u * W;
+    // Where vector u of a key starts, and a pair's second one.
+    auto place = [&](int u, int &d0, int &d1) {
+        d0 = d1 = a.rot / 2 + u * W;
+        if (u * W < a.rot / 2) pair_at<W, INTER>(u, a.rot, d0, d1);
+    };
+    int d0, d1;
+    place(u, d0, d1);
+    const int v0 = share * (int)a.vecs.d, vecs = min((int)a.vecs.d, a.all_vecs - v0);
 
     auto angles = [&](int r0, int r1) {  // of slots [r0, r1)
-        for (int i = tid; i < (r1 - r0) * (a.rot / 2); i += 256) {
-            const int r = (uint32_t)i / a.half, t = r0 + r + t_off;
-            table[i] = rope_angle(a.positions ? a.positions[t] : j * B.block + r0 + r, a.freq[i - r * (int)a.half.d], 1.0f,
-                                  a.amplitude);
+        if (u0 * W >= a.rot / 2) return;
+        for (int i = tid; i < (r1 - r0) * (int)a.half.d; i += 256) {
+            const int r = (uint32_t)i / a.half, t = r0 + r + t_off, f = u0 * W + i - r * (int)a.half.d;
+            if (f < a.rot / 2)
+                table[i] = rope_angle(a.positions ? a.positions[t] : j * B.block + r0 + r, a.freq[f], 1.0f, a.amplitude);
         }
     };
     const bool once = s1 - s0 <= a.rows;
@@ -203,9 +213,10 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
         const int64_t base = ((int64_t)page * a.heads + h) * B.block * a.dim;
         T *kc = (T *)a.k_cache + base, *vc = (T *)a.v_cache + base;
         // Values: copied.
-        const int nv = (s1 - s0) * (int)a.vecs.d;
+        const int nv = vecs > 0 ? (s1 - s0) * (int)a.vecs.d : 0;
         for (int i = tid; i < nv; i += 256) {
-            const int r = (uint32_t)i / a.vecs, c = (i - r * (int)a.vecs.d) * W;
+            // (Behind a part's last vector: that again.)
+            const int r = (uint32_t)i / a.vecs, c = (v0 + min(i - r * (int)a.vecs.d, vecs - 1)) * W;
             const V x = *reinterpret_cast<const V *>((const T *)a.v + (int64_t)(s0 + r + t_off) * a.v_token + h * a.v_head + c);
             __builtin_nontemporal_store(x, reinterpret_cast<V *>(vc + (int64_t)(s0 + r) * a.dim + c));
         }
@@ -220,16 +231,16 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
                 angles(n0, n1);
             }
             __syncthreads();
-            if (g >= groups) continue;
+            if (!mine) continue;
             for (int r = (n0 > s0 ? n0 : a.sums ? 0 : s0) + g; r < n1; r += groups) {
                 T *dst = kc + (int64_t)r * a.dim;
                 const T *src = r < s0 ? dst : (const T *)a.k + (int64_t)(r + t_off) * a.k_token + h * a.k_head;
-                Floats<W> p = load_floats<T, W>(src + d0), q = load_floats<T, W>(src + (pair ? d1 : d0));
+                Floats<W> p = load_floats<T, W>(src + d0), q = load_floats<T, W>(src + d1);
                 if (r >= s0) {
                     if (pair) {
                         CosSin m[W];
 #pragma unroll
-                        for (int k = 0; k < W; ++k) m[k] = table[(r - n0) * (int)a.half.d + u * W + k];
+                        for (int k = 0; k < W; ++k) m[k] = table[(r - n0) * (int)a.half.d + ul * W + k];
                         rotate<W, INTER>(p, q, m);
                         q = store_floats<T, W>(dst + d1, q);
                     }
@@ -243,19 +254,25 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
             }
         }
         if (a.sums == nullptr) continue;
-        if (g < groups) {
+        const int first = units * W, row = 2 * first;  // the first vectors of all units, then the second ones
+        if (mine) {
 #pragma unroll
             for (int i = 0; i < W; ++i) {
-                part[g * a.dim + d0 + i] = sum0.v[i];
-                if (pair) part[g * a.dim + d1 + i] = sum1.v[i];
+                part[g * row + ul * W + i] = sum0.v[i];
+                if (pair) part[g * row + first + ul * W + i] = sum1.v[i];
             }
         }
         __syncthreads();
         float *sums = a.sums + ((int64_t)page * a.heads + h) * a.dim;
-        for (int d = tid; d < a.dim; d += 256) {
+        for (int x = tid; x < row; x += 256) {
+            const bool second = x >= first;
+            const int v = u0 + (x - (second ? first : 0)) / W;
+            if (v >= a.all_units || (second && v * W >= a.rot / 2)) continue;  // (a copied vector has no second)
             float t = 0.0f;
-            for (int k = 0; k < groups; ++k) t += part[k * a.dim + d];
-            sums[d] = t;
+            for (int k = 0; k < groups; ++k) t += part[k * row + x];
+            int e0, e1;
+            place(v, e0, e1);
+            sums[(second ? e1 : e0) + x % W] = t;
         }
         __syncthreads();
     }
@@ -302,16 +319,24 @@ int rope_of(RopeArgs &a, bool inter, hipStream_t stream) {
 
 template <typename T, int W>
 int launch_append(AppendArgs &a, bool inter, hipStream_t stream) {
-    a.units = make_div((uint32_t)((a.dim - a.rot / 2) / W));
-    a.vecs = make_div((uint32_t)(a.dim / W));
-    a.half = make_div((uint32_t)std::max(a.rot / 2, 1));
-    a.rows = std::min(kTable / std::max(a.rot / 2, 1), a.B.q_start ? a.B.block : 1);
-    a.table_len = a.rows * (a.rot / 2);
-    const size_t lds = a.table_len * sizeof(CosSin) + (a.sums ? 256 / a.units.d * a.dim * sizeof(float) : 0);
+    a.all_units = (a.dim - a.rot / 2) / W;
+    a.all_vecs = a.dim / W;
     // Heads a workgroup takes: as many as leave four workgroups for every CU.
     a.each = (int)std::min<int64_t>(std::max<int64_t>(a.items * a.heads / 1024, 1), a.heads);
     a.head_groups = make_div((uint32_t)((a.heads + a.each - 1) / a.each));
-    const dim3 grid = grid_of(a.items * a.head_groups.d);
+    // Parts of the components: as many as leave two workgroups for every CU, and pieces of 64 bytes of a key.
+    const int64_t items = a.items * a.head_groups.d;
+    const int least = std::max(64 / (W * (int)sizeof(T)), 1);
+    const int64_t parts = std::max<int64_t>(std::min<int64_t>(512 / items, a.all_units / least), 1);
+    a.units = make_div((uint32_t)((a.all_units + parts - 1) / parts));
+    a.parts = make_div((uint32_t)((a.all_units + a.units.d - 1) / a.units.d));
+    a.vecs = make_div((uint32_t)((a.all_vecs + a.parts.d - 1) / a.parts.d));
+    const int pairs = std::min((int)a.units.d * W, a.rot / 2);
+    a.half = make_div((uint32_t)std::max(pairs, 1));
+    a.rows = std::min(kTable / std::max(pairs, 1), a.B.q_start ? a.B.block : 1);
+    a.table_len = a.rows * pairs;
+    const size_t lds = a.table_len * sizeof(CosSin) + (a.sums ? 256 / a.units.d * a.units.d * 2 * W * sizeof(float) : 0);
+    const dim3 grid = grid_of(items * a.parts.d);
     if (inter)
         append_kernel<T, W, true><<<grid, 256, lds, stream>>>(a);
     else
@@ -398,7 +423,7 @@ extern "C" int spconv_cache_append(int dtype, const spconv_batch *batch, const v
         batch->q_start ? batch->tokens / batch->block + 2 * (int64_t)batch->sequences : (int64_t)batch->sequences;
     if (items * heads > 0x7fffffff) return SPCONV_EINVAL;
     AppendArgs a{*batch, k, v, k_token, k_head, v_token, v_head, k_cache, v_cache, sums, positions, freq, items, heads,
-                 dim, rot, 1, 1, 0, {}, {}, {}, {}, amplitude};
+                 dim, rot, 1, 1, 0, 0, 0, {}, {}, {}, {}, {}, amplitude};
     const bool inter = (flags & SPCONV_ROPE_INTERLEAVED) != 0;
     if (dtype == SPCONV_F32) return append_of<float>(a, inter, stream);
     if (dtype == SPCONV_F16) return append_of<_Float16>(a, inter, stream);

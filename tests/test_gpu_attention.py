@@ -167,6 +167,39 @@ def test_append(dtype, lens, kv, block, heads, dim, rot, inter):
         near(sums, want, size * block * O.U32, "sums")
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("dim,rot,inter", [(192, 192, True), (256, 168, False), (200, 0, False), (128, 26, True), (256, 2, False), (72, 64, False)])
+def test_append_of_few_heads(dtype, dim, rot, inter):
+    """Pages whose components several workgroups share: cache and sums against the formula, whole pages and part ones."""
+    rng = np.random.default_rng(dim + rot)
+    s = Setup(rng, [100, 3], [130, 40], 64, 1, dim, dtype, tail=1)
+    k, v = (normal(rng, (s.tokens, 1, dim), dtype) for _ in range(2))
+    freq = 500.0 ** (-np.arange(0, rot, 2) / max(rot, 1))
+    kc, vc = s.k.clone(), s.v.clone()
+    sums = torch.full((s.pages, 1, dim), 7.0, device=DEV)
+    A.spconv_cache_append(k, v, kc, vc, s.batch, sums, torch.from_numpy(freq).to(DEV) if rot else None, inter)
+    want_k, want_v = f64(s.k), f64(s.v)
+    bound = np.zeros_like(want_k)
+    touched = {}
+    for b in range(2):
+        n, kv, t0 = int(s.lens[b]), int(s.kv[b]), int(s.start[b])
+        pos = np.arange(kv - n, kv).astype(np.int32)
+        new = O.rope(f64(k)[t0:t0 + n], pos, freq, inter, False, 1.0)
+        off = O.rope_bound(f64(k)[t0:t0 + n], freq, inter, 1.0, dtype, new)
+        for i, p in enumerate(pos):
+            page = int(s.table[b, p // 64])
+            want_k[page, 0, p % 64], bound[page, 0, p % 64], want_v[page, 0, p % 64] = new[i, 0], off[i, 0], f64(v)[t0 + i, 0]
+            touched[page] = min(kv - p // 64 * 64, 64)
+    near(kc, want_k, bound)
+    assert np.array_equal(f64(vc), want_v)
+    for page in range(s.pages):
+        if page not in touched:
+            assert (sums[page] == 7.0).all()
+            continue
+        keys = f64(kc)[page, 0, :touched[page]]  # as stored: 64 fp32 additions at most
+        near(sums[page, 0], keys.sum(0), np.abs(keys).sum(0) * 64 * 2.0 ** -24, page)
+
+
 def test_append_again_after_dropped_tokens():
     """Drafted tokens that are dropped leave no trace in the sums."""
     rng = np.random.default_rng(3)
