@@ -228,7 +228,9 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && NC <= 4 ? 2 : 1) void rows_k
     constexpr int kJoin = 16 * (DP + 4) * 4;
     constexpr int kPerWave = kTile > kJoin ? kTile : kJoin;
     // Addresses are formed anew for each tile where registers are short (fp32, 256 components: 128 -> 107 us; others lose 2%).
+    // There the queries lie in LDS as well.
     constexpr bool kFresh = NC == 8 && sizeof(T) == 4;
+    __shared__ __attribute__((aligned(16))) T q_lds[kFresh ? 16 * (DP + 4) : 1];
     __shared__ __attribute__((aligned(16))) char lds[4 * kPerWave];
     __shared__ Slabs S;
     __shared__ float w_max[4][16], w_sum[4][16];
@@ -244,21 +246,29 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && NC <= 4 ? 2 : 1) void rows_k
     // Query of this lane's column.
     const int m = P.m0 + col, tok = (uint32_t)m / a.group_div;
     const int pos = tok < P.r.n ? P.r.p0 + tok : -1;
-    frag_t<T> q[NC];
+    frag_t<T> q[kFresh ? 1 : NC];
     {
         const T *src = (const T *)a.q + (int64_t)(P.r.t0 + tok) * a.q_token +
                        (int64_t)(P.h * a.group + (m - tok * a.group)) * a.q_head;
 #pragma unroll
         for (int k = 0; k < NC; ++k) {
             const int d = k * 32 + part * 8;
-            q[k] = zero_frag<T>();
+            frag_t<T> x = zero_frag<T>();
             if (tok < P.r.n && d < D) {
                 if (a.q_aligned) {
-                    q[k] = *reinterpret_cast<const frag_t<T> *>(src + d);
+                    x = *reinterpret_cast<const frag_t<T> *>(src + d);
                 } else {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) q[k][i] = src[d + i];
+                    for (int i = 0; i < 8; ++i) x[i] = src[d + i];
                 }
+            }
+            if constexpr (kFresh) {
+                if (wave == 0) {  // (read behind the first barrier of the walk)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) q_lds[col * (DP + 4) + d + i] = x[i];
+                }
+            } else {
+                q[k] = x;
             }
         }
     }
@@ -324,12 +334,30 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && NC <= 4 ? 2 : 1) void rows_k
             f32x4 x[2];
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-                x[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                // fp32 products in chains of 64 components or less: the sum's own roundings grow with a chain's length.
+                constexpr int kChain = sizeof(T) == 2 ? NC : NC == 2 ? 1 : 2;
 #pragma unroll
-                for (int k = 0; k < NC; ++k) {
-                    frag_t<T> f = kf[t][k];
-                    if (k * 32 + part * 8 >= D) f = zero_frag<T>();
-                    x[t] = mma(f, q[k], x[t]);
+                for (int k0 = 0; k0 < NC; k0 += kChain) {
+                    f32x4 sum4 = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                    for (int k = k0; k < k0 + kChain; ++k) {
+                        frag_t<T> f = kf[t][k];
+                        if (k * 32 + part * 8 >= D) f = zero_frag<T>();
+                        if constexpr (kFresh) {
+                            union {
+                                V h[2];
+                                frag_t<T> f;
+                            } u;
+                            const V *at = reinterpret_cast<const V *>(q_lds + col * (DP + 4) + k * 32 + part * 8);
+                            u.h[0] = at[0];
+                            u.h[1] = at[1];
+                            sum4 = mma(f, u.f, sum4);
+                        } else {
+                            sum4 = mma(f, q[k], sum4);
+                        }
+                    }
+                    x[t] = k0 == 0 ? sum4 : x[t] + sum4;
+                    if (NC > 4 && sizeof(T) == 4) __builtin_amdgcn_sched_barrier(0);  // (short of registers)
                 }
             }
             if (s + 8 < n_slabs) fetch_keys(s + 8);
