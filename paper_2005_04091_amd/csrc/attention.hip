@@ -217,8 +217,8 @@ __device__ __forceinline__ int row_unit(int r, int c) {
 // at the end; shares of a row (splits) are joined by join_kernel. NK*32 components are laid out, NC*32 computed.
 // The keys are read once for 16 pairs, so single tokens are bound by HBM: 64 tokens, 8 heads of 4 queries, 128
 // components, bf16, lists of 2048 keys, 97 us, 5.5 TB/s. Two workgroups a CU (one of more than 128 components, whose
-// tiles fill the registers): 16 tokens, 4 heads of 8 queries, 256 components, 42 us, 3.2 TB/s; fp32 108 us, 2.5 TB/s,
-// some of it in scratch memory. Lists of prompts that come from the caches: 1000 rows of one token, 4 heads of 4
+// tiles fill the registers): 16 tokens, 4 heads of 8 queries, 256 components, 42 us, 3.2 TB/s; fp32 92 us, 2.9 TB/s.
+// Lists of prompts that come from the caches: 1000 rows of one token, 4 heads of 4
 // queries, 512 keys, 117 us, 9 TB/s.
 template <typename T, int NK, int NC>
 __global__ __launch_bounds__(256, sizeof(T) == 2 && NC <= 4 ? 2 : 1) void rows_kernel(AttnArgs a) {
@@ -227,8 +227,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && NC <= 4 ? 2 : 1) void rows_k
     constexpr int kTile = 32 * DP * (int)sizeof(T);
     constexpr int kJoin = 16 * (DP + 4) * 4;
     constexpr int kPerWave = kTile > kJoin ? kTile : kJoin;
-    // Addresses are formed anew for each tile where registers are short (fp32, 256 components: 128 -> 107 us; others lose 2%).
-    // There the queries lie in LDS as well.
+    // Addresses are formed anew for each tile where registers are short (fp32, 256 components: 128 -> 107 us; others lose
+    // 2%), and there the queries lie in LDS (-> 92 us).
     constexpr bool kFresh = NC == 8 && sizeof(T) == 4;
     __shared__ __attribute__((aligned(16))) T q_lds[kFresh ? 16 * (DP + 4) : 1];
     __shared__ __attribute__((aligned(16))) char lds[4 * kPerWave];
@@ -1158,7 +1158,7 @@ bool plan_of(int dtype, const spconv_batch *B, int q_heads, int heads, int dim, 
     const int most = dtype == SPCONV_F32 || dim > 128 ? 4 : 8;  // waves of a tile: two a SIMD where registers allow
     p->batch = *B;
     // Without lists rows mean nothing to the result: they are as long as a tile has room for, and sequences tokens.
-    // (two sequences, 1000 tokens, 4 heads of 4 queries and 128 components, rows of one token given: 549 -> 94 us)
+    // (Two sequences, 1000 tokens, 4 heads of 4 queries and 128 components, rows of one token given: 549 -> 66 us.)
     if (keep == 0 && B->q_start) {
         const int64_t tokens = (B->tokens + B->sequences - 1) / B->sequences;
         int q = std::min(std::max(most * 32 / group, 1), 128);
@@ -1172,7 +1172,7 @@ bool plan_of(int dtype, const spconv_batch *B, int q_heads, int heads, int dim, 
     // Rows of more pairs than these are tiles of 32 pairs for each of some waves. (128 components, bf16, 2000 tokens: 16
     // pairs 73 us by rows and 123 by tiles, 32 pairs 74 and 64; fp32 of 64 components, 32 pairs: 86 and 107. Wide ones
     // keep a CU busy with four waves only, of which few pairs leave three or two idle: 32 pairs of 2000 tokens, 256
-    // components, 239 us by tiles and 210 by rows; fp32 1134 and 567, 64 pairs 712 and 562.)
+    // components, 239 us by tiles and 210 by rows; fp32 1134 and 531, 64 pairs 712 and 528.)
     const bool f32 = dtype == SPCONV_F32;
     const int few = dim <= 64 ? (f32 ? 32 : 16) : dim <= 128 ? 16 : f32 ? 64 : dim > 192 ? 32 : 16;
     // (fp32 of more than 192: five and a half tiles of 16 pairs cost one of 128; 132 pairs 615 and 737 us.)

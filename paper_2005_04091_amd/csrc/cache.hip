@@ -155,7 +155,8 @@ struct AppendArgs {
 constexpr int kTable = 4096;  // sines and cosines in LDS at most
 
 // One workgroup a (touched page, group of heads, part of the components: one part where there are enough pages and heads
-// for the GPU; 2254 tokens of 4 sequences, one head of 192, pages of 128 keys: 26 us by one part, 15 by three). The pages that sequence b touches are items
+// for the GPU; 2254 tokens of 4 sequences, one head of 192, pages of 128 keys: 26 us by one part, 15 by three).
+// The pages that sequence b touches are items
 // q_start[b]/block + 2b and on: a sequence of n tokens touches n/block + 2 pages at
 // most. Sines and cosines of the page's new tokens are formed once for the group's heads, in LDS. Threads hold one
 // vector pair of a key each and walk the page's rows in strides, so that the
