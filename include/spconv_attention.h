@@ -52,8 +52,8 @@ extern "C" {
  * Tokens are packed: sequence b has tokens [q_start[b], q_start[b+1]) of the
  * call's `tokens`, the newest of its kv_len[b] keys, so its i-th token stands at
  * position p = kv_len[b] - (q_start[b+1] - q_start[b]) + i and sees the keys
- * 0 .. p. Without q_start every sequence has one token, token b (generation; then
- * tokens must equal sequences).
+ * 0 .. p. Without q_start every sequence has one token, token b, as with
+ * q_start[b] = b (generation; then tokens must equal sequences).
  *
  * Keys lie in pages of `block` keys: key j of sequence b is slot j % block of
  * page table[b*table_stride + j/block].

@@ -1159,6 +1159,7 @@ bool plan_of(int dtype, const spconv_batch *B, int q_heads, int heads, int dim, 
     p->batch = *B;
     // Without lists rows mean nothing to the result: they are as long as a tile has room for, and sequences tokens.
     // (Two sequences, 1000 tokens, 4 heads of 4 queries and 128 components, rows of one token given: 549 -> 66 us.)
+    if (keep == 0 && !B->q_start) p->batch.q_block = 1;
     if (keep == 0 && B->q_start) {
         const int64_t tokens = (B->tokens + B->sequences - 1) / B->sequences;
         int q = std::min(std::max(most * 32 / group, 1), 128);
@@ -1166,7 +1167,7 @@ bool plan_of(int dtype, const spconv_batch *B, int q_heads, int heads, int dim, 
         p->batch.q_block = q;
     }
     B = &p->batch;
-    const int64_t pairs = (int64_t)B->q_block * group;
+    const int64_t pairs = (int64_t)row_tokens(B) * group;
     p->waves = 0;
     p->tile_pairs = 16;
     // Rows of more pairs than these are tiles of 32 pairs for each of some waves. (128 components, bf16, 2000 tokens: 16

@@ -3,6 +3,7 @@
 #pragma once
 
 #include "common.h"
+#include "rows.h"
 #include "spconv_attention.h"
 
 #include <cmath>
@@ -112,11 +113,12 @@ __device__ __forceinline__ Seq find_seq(const spconv_batch &B, int x, int div, i
     Seq s;
     const int tokens = (int)B.tokens;
     x = uniform(x);
-    if (B.q_start == nullptr) {
-        s.b = x;
+    if (B.q_start == nullptr) {  // one item each
+        s.b = x < B.sequences ? x : -1;
         s.first = x;
-        s.n = 1;
-        s.at = 0;
+        s.n = s.b < 0 ? 0 : 1;
+        s.at = s.kv = 0;
+        if (s.b < 0) return s;
     } else {
         const int lane = threadIdx.x & (kWave - 1);
         s.b = 0;
@@ -151,6 +153,10 @@ struct Row {
 };
 
 __device__ __forceinline__ Row find_row(const spconv_batch &B, int row) {
+    if (B.q_start == nullptr) {
+        const Seq s = find_seq(B, sequence_of_row(uniform(row), B.q_block, B.sequences), 1, 0);
+        return {s.b, s.first, s.n, s.kv - 1, s.kv};
+    }
     const Seq s = B.q_block == 1 ? find_seq(B, row, 1, 0) : find_seq(B, row, B.q_block, 1);
     Row r{s.b, 0, 0, 0, s.kv};
     if (s.b < 0 || s.at < 0) return r;
@@ -184,6 +190,9 @@ inline bool batch_arrays_ok(const spconv_batch *B) { return B->table != nullptr 
 inline int64_t rows_of(const spconv_batch *B) {
     return B->q_block == 1 ? B->tokens : B->tokens / B->q_block + B->sequences;
 }
+
+// Tokens that a row has at most.
+inline int row_tokens(const spconv_batch *B) { return B->q_start ? B->q_block : 1; }
 
 inline bool dtype_ok(int dtype) { return dtype == SPCONV_F32 || dtype == SPCONV_F16 || dtype == SPCONV_BF16; }
 

@@ -667,7 +667,7 @@ int scores_of(const ScoreArgs &a, hipStream_t stream) {
 
 template <typename T>
 int scores_by_pairs(const ScoreArgs &a, hipStream_t stream) {
-    return a.B.q_block * a.group <= 16 ? scores_of<T, true>(a, stream) : scores_of<T, false>(a, stream);
+    return row_tokens(&a.B) * a.group <= 16 ? scores_of<T, true>(a, stream) : scores_of<T, false>(a, stream);
 }
 
 }  // namespace
@@ -678,7 +678,7 @@ extern "C" int spconv_block_scores(int dtype, const spconv_batch *batch, const v
     if (!batch_ok(batch) || !batch_arrays_ok(batch) || !dtype_ok(dtype) || q == nullptr || sums == nullptr ||
         scores == nullptr || !heads_ok(q_heads, heads, dim) || q_token < 0 || q_head < 0 || !aligned16(sums))
         return SPCONV_EINVAL;
-    const int per = score_blocks((int64_t)batch->q_block * (q_heads / std::max(heads, 1)) <= 16);
+    const int per = score_blocks(row_tokens(batch) * (q_heads / heads) <= 16);
     const int tiles = (batch->max_blocks + per - 1) / per;
     const int64_t rows = rows_of(batch);
     if (rows * heads * tiles >= ((int64_t)1 << 31)) return SPCONV_EINVAL;

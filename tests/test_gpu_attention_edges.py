@@ -1,0 +1,75 @@
+"""GPU tests of the attention calls where sizes and values meet that a step seldom has at once: rows of several tokens for
+single tokens, values that are not finite beside keys that are masked, far positions. The forms and bounds are
+attention_oracle.py's; infinities and NaN have to come out as themselves."""
+import numpy as np
+import pytest
+import torch
+
+import attention_oracle as O
+import test_gpu_attention as T
+from paper_2005_04091_amd import attention as A
+
+pytestmark = pytest.mark.gpu
+TYPES, DEV, f64, normal, Setup, random_lists = T.TYPES, T.DEV, T.f64, T.normal, T.Setup, T.random_lists
+
+
+def near(got, want, bound, what=""):
+    """Finite numbers within the bound; infinities of the same sign and NaN where those are due, and nowhere else."""
+    got = f64(got) if isinstance(got, torch.Tensor) else got
+    odd = ~np.isfinite(want)
+    with np.errstate(invalid="ignore"):
+        fine = np.where(odd, (got == want) | (np.isnan(got) & np.isnan(want)), np.abs(got - want) <= bound)
+    assert fine.all(), (what, int((~fine).sum()), got[~fine][:4], want[~fine][:4], np.argwhere(~fine)[:4])
+
+
+def check_attention(s, q, heads, blocks=None, counts=None, scale=None):
+    """Outputs between guards, against the formula."""
+    dev = lambda a: None if a is None else torch.from_numpy(a).to(DEV)
+    n, D = q.shape[0], q.shape[2]
+    out = torch.full((n + 256, *q.shape[1:]), 3.0, dtype=q.dtype, device=DEV)
+    lse = torch.full((n + 256, q.shape[1]), 3.0, device=DEV)
+    A.spconv_block_attention(q, s.k, s.v, s.batch, dev(blocks), dev(counts), scale, out[128:-128], lse[128:-128])
+    wo, wl, bo, bl = O.attention(s.rows, f64(q), f64(s.k), f64(s.v), s.table, s.block, D ** -0.5 if scale is None else scale, blocks,
+                                 counts, q.dtype)
+    mine = np.zeros(n + 256, bool)
+    for _, toks, _ in s.rows.of.values():
+        mine[[t + 128 for t in toks]] = True
+    assert (f64(out)[~mine] == 3.0).all() and (f64(lse)[~mine] == 3.0).all()
+    some = mine[128:-128]
+    near(f64(out)[mine], wo[some], bo[some], "out")
+    near(f64(lse)[mine], wl[some], bl[some], "lse")
+    return out[128:-128], lse[128:-128]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("B,q_block,group", [(1, 2, 4), (3, 2, 1), (64, 16, 4), (70, 4, 20), (5, 128, 4), (200, 8, 2), (17, 16, 8)])
+def test_single_tokens_in_rows_of_several(dtype, B, q_block, group):
+    """Without q_start sequence b is token b of row b/q_block + b; the rows between and behind have no tokens."""
+    rng = np.random.default_rng(B * 131 + q_block)
+    s = Setup(rng, [1] * B, rng.integers(0, 300, B), 16, 2, 64, dtype, q_block, decode=True)
+    q = normal(rng, (B, 2 * group, 64), dtype)
+    all_keys = check_attention(s, q, 2)
+    blocks, counts = random_lists(rng, s, 2, 6)
+    check_attention(s, q, 2, blocks, counts)
+    sums = normal(rng, (s.pages, 2, 64), torch.float32, 3.0)
+    want, bound = O.scores(s.rows, f64(q), f64(sums), s.table, s.kv, 16, 2)
+    got = A.spconv_block_scores(q, sums, s.batch)
+    near(got, want, bound, "scores")
+    keep = 2 + -(-(q_block - 1) // 16)
+    wb, wc = O.select(s.rows, f64(got), 16, keep, 1, 1)
+    blocks, counts = A.spconv_select_blocks(got, s.batch, keep)
+    assert np.array_equal(blocks.cpu().numpy(), wb) and np.array_equal(counts.cpu().numpy(), wc)
+    check_attention(s, q, 2, wb, wc)
+    # Nothing of it depends on q_block where there are no lists.
+    one = A.CacheBatch(s.batch.table, s.batch.kv_len, 16)
+    assert all(torch.equal(a, b) for a, b in zip(all_keys, A.spconv_block_attention(q, s.k, s.v, one, lse=True)))
+    # The append: a token's key and value to its sequence's newest slot.
+    k, v = (normal(rng, (B, 2, 64), dtype) for _ in range(2))
+    kc, vc, sums = s.k.clone(), s.v.clone(), torch.zeros((s.pages, 2, 64), device=DEV)
+    A.spconv_cache_append(k, v, kc, vc, s.batch, sums)
+    want_k, want_v = s.k.clone(), s.v.clone()
+    for b in range(B):
+        if s.kv[b]:
+            at = int(s.table[b, (s.kv[b] - 1) // 16]), slice(None), int(s.kv[b] - 1) % 16
+            want_k[at], want_v[at] = k[b], v[b]
+    assert torch.equal(kc, want_k) and torch.equal(vc, want_v)
