@@ -448,10 +448,11 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && NC <= 4 ? 2 : 1) void rows_k
                 o[t] = mma(f, w, o[t]);
             }
             if (__ballot(odd)) {
-                // Values that are not finite, in a tile of which some queries see a part only: one by one.
+                // Values that are not finite, in a tile of which some queries see a part only: one by one, those of the
+                // half that all see too (both halves were cleaned).
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
-                    if (!there[t] || key0[t] + 15 <= first_pos) continue;
+                    if (!there[t]) continue;
                     for (int kr = 0; kr < 16; ++kr) {
                         if (key0[t] + kr > pos) continue;
                         const T *src = (const T *)a.v_cache + S.base[s + t] + kr * D;

@@ -73,3 +73,44 @@ def test_single_tokens_in_rows_of_several(dtype, B, q_block, group):
             at = int(s.table[b, (s.kv[b] - 1) // 16]), slice(None), int(s.kv[b] - 1) % 16
             want_k[at], want_v[at] = k[b], v[b]
     assert torch.equal(kc, want_k) and torch.equal(vc, want_v)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("dim", [64, 128, 192, 256])
+@pytest.mark.parametrize("q_block", [1, 3, 16])
+def test_values_that_are_not_finite_beside_masked_keys(dtype, dim, q_block):
+    """Infinities and NaN of values that a query sees come out, also where the block beside theirs in a tile is seen in part,
+    is no block, has no page, or where the list ends behind theirs; those that it does not see stay out."""
+    rng = np.random.default_rng(dim + q_block)
+    s = Setup(rng, [6, 21], [90, 120], 16, 2, dim, dtype, q_block, extra_cols=1)
+    s.table[1, 4] = -1
+    s.make()
+    for b in range(2):
+        for pos, d, x in [(70, 1, "nan"), (65, 3, "inf"), (74, dim - 1, "-inf"), (10, 9, "inf"), (85, 11, "nan"), (87, 13, "-inf"),
+                          (50, 5, "inf"), (30, 7, "nan")]:
+            page = int(s.table[b, pos // 16])
+            if page >= 0:
+                s.v[page, pos % 2, pos % 16, d] = float(x)
+    q = normal(rng, (s.tokens, 8, dim), dtype)
+    check_attention(s, q, 2)
+    lists = np.array([[4, 5, -1], [0, -1, 5], [4, -1, -1], [1, 5, 2], [3, 0, 4], [-1, 3, 4], [5, 4, 3], [4, 3, 0], [6, 7, 2]], np.int32)
+    blocks = np.stack([np.stack([lists[(r * 2 + h) % len(lists)] for h in range(2)]) for r in range(s.rows.rows)])
+    check_attention(s, q, 2, blocks)
+    counts = (np.arange(s.rows.rows * 2, dtype=np.int32) % 4).reshape(-1, 2)
+    check_attention(s, q, 2, blocks, counts)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("kv", [17, 90, 1000, 5000])
+def test_an_infinite_value_anywhere(dtype, kv):
+    """A token of a generating sequence sees every key of its cache: the one infinite value comes out wherever it lies, and in
+    its own component alone (rows of one share and of many)."""
+    rng = np.random.default_rng(kv)
+    s = Setup(rng, [1], [kv], 16, 1, 64, dtype, decode=True)
+    q = normal(rng, (1, 4, 64), dtype)
+    for key in sorted({0, 15, kv // 2, max(kv - 33, 0), max(kv - 17, 0), kv - 2, kv - 1}):
+        at = int(s.table[0, key // 16]), 0, key % 16, key % 64
+        was = s.v[at].clone()
+        s.v[at] = float("-inf") if key % 2 else float("inf")
+        check_attention(s, q, 1)
+        s.v[at] = was
