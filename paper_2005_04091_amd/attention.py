@@ -363,6 +363,8 @@ def spconv_block_attention(q, k_cache, v_cache, batch: CacheBatch, blocks=None, 
         if blocks.dim() != 3:
             raise ValueError("blocks must be [rows, heads, keep]")
         keep = blocks.shape[2]
+        if keep == 0:  # (it has no address, which would stand for no lists: all blocks)
+            raise SpconvError(SPCONV_EINVAL, "spconv_block_attention")
         bp = _whole(blocks, "blocks", torch.int32, (batch.rows, H, keep), device)
     if counts is not None:
         cp = _whole(counts, "counts", torch.int32, (batch.rows, H), device)
