@@ -22,7 +22,7 @@
  *
  * Element types (dtype): keys, values, queries and outputs of one call have the
  * same type. Dot products, softmax statistics, sums, scores and partial outputs
- * are fp32, angles fp64; a value is rounded to its type once, when it is stored
+ * are fp32, angles fp64 (their sines and cosines fp32); a value is rounded to its type once, when it is stored
  * (fp16 and bf16 attention rounds the softmax weights to the type as well, for
  * the matrix cores).
  */
@@ -114,7 +114,7 @@ int spconv_rope_frequencies(int rot, double base, const spconv_rope_scaling *sca
 /*
  * spconv_rope - rotary positions (device, asynchronous).
  * For pair i of the first rot components of every head, with angle = positions[t] * freq[i]
- * (fp64; negated with SPCONV_ROPE_INVERSE), c = cos(angle), s = sin(angle):
+ * (rounded to fp64; negated with SPCONV_ROPE_INVERSE), c = cos(angle), s = sin(angle), both fp32, within 2^-22.6:
  *   out1 = amplitude * (x1 c - x2 s),  out2 = amplitude * (x2 c + x1 s);
  * components from rot on are copied.
  * x, out     device; token t, head h, component d at t*token_stride + h*head_stride + d

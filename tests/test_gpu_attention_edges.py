@@ -114,3 +114,18 @@ def test_an_infinite_value_anywhere(dtype, kv):
         s.v[at] = float("-inf") if key % 2 else float("inf")
         check_attention(s, q, 1)
         s.v[at] = was
+
+
+@pytest.mark.parametrize("low,high", [(0, 1 << 20), (1 << 27, 1 << 28), (1 << 30, (1 << 31) - 1), (-(1 << 31), -(1 << 30))])
+def test_rotations_of_far_positions(low, high):
+    """Unit vectors become cosine and sine of the fp64 angle. Those are within two fp32 steps, 2^-23, of exact for the fp32
+    number next to the angle's fraction of a turn, and the correction for the rest is rounded once, 2^-25."""
+    rng = np.random.default_rng(high % 1000)
+    pos = rng.integers(low, high, 4096).astype(np.int32)
+    pos[:2] = low, high - 1
+    freq = np.concatenate([10000.0 ** (-np.arange(0, 32, 2) / 32), [0.999999, 1 / 3, 0.7, 1e-9]])
+    x = torch.zeros((4096, 1, 40), device=DEV)
+    x[:, :, :20] = 1.0
+    y = A.spconv_rope(x, torch.from_numpy(pos).to(DEV), torch.from_numpy(freq).to(DEV))
+    angle = pos.astype(np.float64)[:, None] * freq
+    near(y[:, 0], np.concatenate([np.cos(angle), np.sin(angle)], 1), 2.0 ** -23 + 2.0 ** -25)
