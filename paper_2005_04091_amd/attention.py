@@ -413,10 +413,10 @@ class BlockAttention:
         """Queries rotated by their ``positions``."""
         return spconv_rope(q, positions, self.freq, self.interleaved, amplitude=self.amplitude, out=out, stream=stream)
 
-    def append(self, k, v, batch: CacheBatch, stream=None):
-        """Keys and values of a step into the cache."""
+    def append(self, k, v, batch: CacheBatch, stream=None, positions=None):
+        """Keys and values of a step into the cache, keys rotated by their place in the sequence or by ``positions``."""
         spconv_cache_append(k, v, self.k_cache, self.v_cache, batch, self.sums, self.freq, self.interleaved,
-                            self.amplitude, stream=stream)
+                            self.amplitude, positions, stream=stream)
 
     def select(self, q, batch: CacheBatch, stream=None):
         """(blocks, counts) that the rows of the rotated ``q`` read; (None, None) without a selection."""
@@ -432,9 +432,13 @@ class BlockAttention:
 
     def step(self, q, k, v, positions, batch: CacheBatch, out=None, lse=None, stream=None):
         """One step: ``q`` [tokens, q_heads, dim], ``k`` and ``v`` [tokens, heads, dim] as projected, ``positions`` int32
-        [tokens] of the tokens in their sequences. Returns the attention's output (and log-sum-exp, if asked for)."""
-        if self.freq is not None:
+        [tokens] by which queries and keys are rotated (those of the tokens in their sequences, or others that the model
+        counts in; where keys lie and what a token sees goes by the batch alone). Returns the attention's output (and
+        log-sum-exp, if asked for)."""
+        if self.freq is None:
+            positions = None
+        else:
             q = self.rotate(q, positions, stream=stream)
-        self.append(k, v, batch, stream=stream)
+        self.append(k, v, batch, stream=stream, positions=positions)
         blocks, counts = self.select(q, batch, stream=stream)
         return self.attend(q, batch, blocks, counts, out, lse, stream=stream)

@@ -129,3 +129,31 @@ def test_rotations_of_far_positions(low, high):
     y = A.spconv_rope(x, torch.from_numpy(pos).to(DEV), torch.from_numpy(freq).to(DEV))
     angle = pos.astype(np.float64)[:, None] * freq
     near(y[:, 0], np.concatenate([np.cos(angle), np.sin(angle)], 1), 2.0 ** -23 + 2.0 ** -25)
+
+
+@pytest.mark.parametrize("keep", [0, 6])
+def test_a_step_rotates_queries_and_keys_alike(keep):
+    """Positions that the model counts from elsewhere than the sequence's first key: keys are stored as rotated by them, and
+    the output is that of the scores between them."""
+    rng = np.random.default_rng(71 + keep)
+    dtype, heads, dim, block = torch.float32, 2, 64, 16
+    layer = A.BlockAttention(30, heads, dim, block, keep, dtype=dtype, device=DEV)
+    lens, B = [40, 23], 2
+    s = Setup(rng, lens, lens, block, heads, dim, dtype, 8)
+    q, k, v = (normal(rng, (s.tokens, h, dim), dtype) for h in (2 * heads, heads, heads))
+    pos = np.concatenate([np.arange(n) * (b + 1) + 500 * b + 7 for b, n in enumerate(lens)]).astype(np.int32)
+    dev_pos = torch.from_numpy(pos).to(DEV)
+    out = layer.step(q, k, v, dev_pos, s.batch)
+    freq = f64(layer.freq)
+    want = O.rope(f64(k), pos, freq)
+    bound = O.rope_bound(f64(k), freq, False, 1.0, dtype, want)
+    for b in range(B):
+        for i in range(lens[b]):
+            t = int(s.start[b]) + i
+            near(layer.k_cache[int(s.table[b, i // block]), :, i % block], want[t], bound[t], (b, i))
+    rotated = layer.rotate(q, dev_pos)
+    blocks, counts = layer.select(rotated, s.batch)
+    host = lambda t: None if t is None else t.cpu().numpy()
+    wo, _, bo, _ = O.attention(s.rows, f64(rotated), np.nan_to_num(f64(layer.k_cache)), np.nan_to_num(f64(layer.v_cache)), s.table, block,
+                               dim ** -0.5, host(blocks), host(counts), dtype)
+    near(out, wo, bo)
