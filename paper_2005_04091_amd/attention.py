@@ -9,6 +9,7 @@ strings the calls of one step together.
 
 Queries, keys and outputs are [tokens, heads, dim] tensors with any strides whose
 last is 1; caches are [pages, heads, block, dim], key sums [pages, heads, dim].
+No gradients are recorded: tensors that require them are refused while torch records.
 """
 from __future__ import annotations
 
@@ -83,6 +84,11 @@ def _device(t, name):
     return t.device
 
 
+def _refuse_grad(name):
+    raise ValueError(f"{name} requires grad, and the calls record no gradients: use torch.no_grad() or detach() (the "
+                     "gradient of spconv_rope is the call with inverse=True)")
+
+
 def _rows(t, name, dtype, shape, device):
     """Pointer and strides of a [tokens, heads, dim] tensor of these."""
     if not isinstance(t, torch.Tensor) or t.device != device or t.dtype is not dtype:
@@ -92,6 +98,8 @@ def _rows(t, name, dtype, shape, device):
     a, b, c = t.stride()
     if c != 1 and shape[2] > 1:
         raise ValueError(f"the last dimension of {name} must be contiguous")
+    if t.requires_grad and torch.is_grad_enabled():
+        _refuse_grad(name)
     # A dimension of one element is never stepped over: its stride says nothing.
     return t.data_ptr(), a if shape[0] > 1 else shape[2], b if shape[1] > 1 else shape[2]
 
@@ -102,6 +110,8 @@ def _whole(t, name, dtype, shape, device):
         raise TypeError(f"{name} must be a contiguous {dtype} tensor on {device}")
     if t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.requires_grad and torch.is_grad_enabled():
+        _refuse_grad(name)
     return t.data_ptr()
 
 
@@ -230,6 +240,8 @@ def _freq(freq, device):
     if not isinstance(freq, torch.Tensor) or freq.device != device or freq.dtype is not torch.float64 or freq.dim() != 1 \
             or not freq.is_contiguous():
         raise TypeError(f"freq must be a contiguous one-dimensional float64 tensor on {device}")
+    if freq.requires_grad and torch.is_grad_enabled():
+        _refuse_grad("freq")
     n = freq.numel()
     return (freq.data_ptr(), 2 * n) if n else (None, 0)
 

@@ -23,3 +23,21 @@ def test_empty_lists_are_refused():
     with pytest.raises(A.SpconvError) as e:
         A.spconv_block_attention(q, cache, cache.clone(), host_batch(), torch.zeros((3, 2, 0), dtype=torch.int32))
     assert e.value.code == A.SPCONV_EINVAL
+
+
+def test_tensors_that_require_grad_are_refused():
+    """Their gradients would be lost without a word."""
+    batch, q, cache = host_batch(), torch.zeros(3, 2, 64), torch.zeros(5, 2, 16, 64)
+    grad = lambda t: t.clone().requires_grad_(True)
+    sums, freq, scores = torch.zeros(5, 2, 64), torch.ones(4, dtype=torch.float64), torch.zeros(3, 2, 4)
+    for call in (lambda: A.spconv_cache_append(grad(q), q, cache, cache, batch), lambda: A.spconv_cache_append(q, grad(q), cache, cache, batch),
+                 lambda: A.spconv_cache_append(q, q, grad(cache), cache, batch), lambda: A.spconv_block_scores(grad(q), sums, batch),
+                 lambda: A.spconv_cache_append(q, q, cache, cache, batch, freq=grad(freq)), lambda: A.spconv_block_scores(q, grad(sums), batch), lambda: A.spconv_select_blocks(grad(scores), batch, 4),
+                 lambda: A.spconv_block_attention(grad(q), cache, cache, batch), lambda: A.spconv_block_attention(q, grad(cache), cache, batch),
+                 lambda: A.spconv_block_attention(q, cache, grad(cache), batch)):
+        with pytest.raises(ValueError, match="requires grad"):
+            call()
+    x = grad(q)
+    with torch.no_grad():
+        assert A._rows(x, "x", x.dtype, x.shape, x.device)[0] == A._whole(x, "x", x.dtype, x.shape, x.device) == x.data_ptr()
+    assert A._rows(x.detach(), "x", x.dtype, x.shape, x.device)[0] == x.data_ptr()

@@ -157,3 +157,12 @@ def test_a_step_rotates_queries_and_keys_alike(keep):
     wo, _, bo, _ = O.attention(s.rows, f64(rotated), np.nan_to_num(f64(layer.k_cache)), np.nan_to_num(f64(layer.v_cache)), s.table, block,
                                dim ** -0.5, host(blocks), host(counts), dtype)
     near(out, wo, bo)
+
+
+def test_a_rotation_of_what_requires_grad_is_refused():
+    x = torch.randn((3, 2, 16), device=DEV, requires_grad=True)
+    args = torch.arange(3, dtype=torch.int32, device=DEV), torch.ones(4, dtype=torch.float64, device=DEV)
+    with pytest.raises(ValueError, match="requires grad"):
+        A.spconv_rope(x, *args)
+    with torch.no_grad():
+        assert torch.equal(A.spconv_rope(x, *args), A.spconv_rope(x.detach(), *args))
