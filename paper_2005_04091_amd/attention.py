@@ -122,10 +122,17 @@ def _dtype(t, name):
     return code
 
 
-def _dims3(t, name):
-    if t.dim() != 3:
-        raise ValueError(f"{name} must be [tokens, heads, dim]")
+def _dims(t, name, what):
+    """Shape of a tensor of such dimensions."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a tensor")
+    if t.dim() != len(what):
+        raise ValueError(f"{name} must be [{', '.join(what)}]")
     return t.shape
+
+
+_QUERIES = ("tokens", "heads", "dim")
+_CACHE = ("pages", "heads", "block", "dim")
 
 
 class _Here:
@@ -251,7 +258,7 @@ def spconv_rope(x, positions, freq, interleaved: bool = False, inverse: bool = F
     """``x`` [tokens, heads, dim] rotated by ``positions`` (int32 [tokens]) in its first 2*len(``freq``) components.
     ``inverse`` undoes it (and is its gradient, with the same amplitude). ``out`` may be ``x``."""
     device = _device(x, "x")
-    T, H, D = _dims3(x, "x")
+    T, H, D = _dims(x, "x", _QUERIES)
     code = _dtype(x, "x")
     xp, xt, xh = _rows(x, "x", x.dtype, (T, H, D), device)
     pp = _whole(positions, "positions", torch.int32, (T,), device)
@@ -266,9 +273,7 @@ def spconv_rope(x, positions, freq, interleaved: bool = False, inverse: bool = F
 
 
 def _cache(k_cache, v_cache, batch, heads, dim, dtype, device):
-    if k_cache.dim() != 4:
-        raise ValueError("k_cache must be [pages, heads, block, dim]")
-    shape = (k_cache.shape[0], heads, batch.block, dim)
+    shape = (_dims(k_cache, "k_cache", _CACHE)[0], heads, batch.block, dim)
     return _whole(k_cache, "k_cache", dtype, shape, device), _whole(v_cache, "v_cache", dtype, shape, device), shape[0]
 
 
@@ -277,7 +282,7 @@ def spconv_cache_append(k, v, k_cache, v_cache, batch: CacheBatch, sums=None, fr
     """Store the step's ``k`` and ``v`` [tokens, heads, dim] in the cache (keys rotated on the way with ``freq``, by their
     place in the sequence or by ``positions``) and set ``sums`` of the pages that got keys."""
     device = batch.device
-    T, H, D = _dims3(k, "k")
+    T, H, D = _dims(k, "k", _QUERIES)
     if T != batch.tokens:
         raise ValueError(f"k has {T} tokens, the batch {batch.tokens}")
     code = _dtype(k, "k")
@@ -297,12 +302,10 @@ def spconv_block_scores(q, sums, batch: CacheBatch, out=None, stream=None):
     """Scores [rows, heads, blocks] of every block of the cache for every row of ``q`` [tokens, q_heads, dim], by the
     blocks' key ``sums`` [pages, heads, dim]."""
     device = batch.device
-    T, HQ, D = _dims3(q, "q")
+    T, HQ, D = _dims(q, "q", _QUERIES)
     if T != batch.tokens:
         raise ValueError(f"q has {T} tokens, the batch {batch.tokens}")
-    if sums.dim() != 3:
-        raise ValueError("sums must be [pages, heads, dim]")
-    pages, H, _ = sums.shape
+    pages, H, _ = _dims(sums, "sums", ("pages", "heads", "dim"))
     code = _dtype(q, "q")
     qp, qt, qh = _rows(q, "q", q.dtype, (T, HQ, D), device)
     sp = _whole(sums, "sums", torch.float32, (pages, H, D), device)
@@ -321,9 +324,7 @@ def spconv_select_blocks(scores, batch: CacheBatch, keep: int, sink: int = 1, lo
     them: the first ``sink``, the row's own and the ``local`` - 1 before them, and the best scored others. ``out``: such a
     pair to write into."""
     device = batch.device
-    if scores.dim() != 3:
-        raise ValueError("scores must be [rows, heads, blocks]")
-    H = scores.shape[1]
+    H = _dims(scores, "scores", ("rows", "heads", "blocks"))[1]
     sp = _whole(scores, "scores", torch.float32, (batch.rows, H, batch.max_blocks), device)
     with _on(device, stream) as raw:
         if out is None:
@@ -361,20 +362,16 @@ def spconv_block_attention(q, k_cache, v_cache, batch: CacheBatch, blocks=None, 
     lse). ``workspace``: a uint8 tensor of ``spconv_attention_workspace`` bytes; without it one is allocated on the stream.
     Tokens that no sequence has are left as they are (in new outputs: unset)."""
     device = batch.device
-    T, HQ, D = _dims3(q, "q")
+    T, HQ, D = _dims(q, "q", _QUERIES)
     if T != batch.tokens:
         raise ValueError(f"q has {T} tokens, the batch {batch.tokens}")
-    if k_cache.dim() != 4:
-        raise ValueError("k_cache must be [pages, heads, block, dim]")
-    H = k_cache.shape[1]
+    H = _dims(k_cache, "k_cache", _CACHE)[1]
     code = _dtype(q, "q")
     qp, qt, qh = _rows(q, "q", q.dtype, (T, HQ, D), device)
     kc, vc, pages = _cache(k_cache, v_cache, batch, H, D, q.dtype, device)
     keep, bp, cp = 0, None, None
     if blocks is not None:
-        if blocks.dim() != 3:
-            raise ValueError("blocks must be [rows, heads, keep]")
-        keep = blocks.shape[2]
+        keep = _dims(blocks, "blocks", ("rows", "heads", "keep"))[2]
         if keep == 0:  # (it has no address, which would stand for no lists: all blocks)
             raise SpconvError(SPCONV_EINVAL, "spconv_block_attention")
         bp = _whole(blocks, "blocks", torch.int32, (batch.rows, H, keep), device)

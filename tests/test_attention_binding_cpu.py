@@ -41,3 +41,17 @@ def test_tensors_that_require_grad_are_refused():
     with torch.no_grad():
         assert A._rows(x, "x", x.dtype, x.shape, x.device)[0] == A._whole(x, "x", x.dtype, x.shape, x.device) == x.data_ptr()
     assert A._rows(x.detach(), "x", x.dtype, x.shape, x.device)[0] == x.data_ptr()
+
+
+def test_what_is_no_tensor_is_a_type_error():
+    batch, q, cache = host_batch(), torch.zeros(3, 2, 64), torch.zeros(5, 2, 16, 64)
+    for call in (lambda: A.spconv_cache_append(None, q, cache, cache, batch), lambda: A.spconv_cache_append(q, q, [1], cache, batch),
+                 lambda: A.spconv_block_scores([[1.0]], cache[:, :, 0], batch), lambda: A.spconv_block_scores(q, None, batch),
+                 lambda: A.spconv_select_blocks(None, batch, 4), lambda: A.spconv_block_attention("q", cache, cache, batch),
+                 lambda: A.spconv_block_attention(q, None, cache, batch), lambda: A.spconv_block_attention(q, cache, cache, batch, [[[0]]])):
+        with pytest.raises(TypeError):
+            call()
+    with pytest.raises(ValueError, match="tokens, heads, dim"):
+        A.spconv_block_attention(q[0], cache, cache, batch)
+    with pytest.raises(ValueError, match="pages, heads, block, dim"):
+        A.spconv_block_attention(q, cache[0], cache, batch)
