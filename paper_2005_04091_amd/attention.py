@@ -350,6 +350,8 @@ def _workspace(code, sequences, block, max_blocks, q_block, tokens, one_each, q_
 
 def spconv_attention_workspace(dtype, batch: CacheBatch, q_heads: int, heads: int, dim: int, keep: int = 0) -> int:
     """Bytes of scratch memory of a ``spconv_block_attention`` call of these sizes."""
+    if dtype not in _DTYPES:
+        raise TypeError(f"dtype must be float32, float16 or bfloat16, not {dtype}")
     return _workspace(_DTYPES[dtype], batch.sequences, batch.block, batch.max_blocks, batch.q_block, batch.tokens,
                       batch.q_start is None, q_heads, heads, dim, keep)
 

@@ -55,3 +55,9 @@ def test_what_is_no_tensor_is_a_type_error():
         A.spconv_block_attention(q[0], cache, cache, batch)
     with pytest.raises(ValueError, match="pages, heads, block, dim"):
         A.spconv_block_attention(q, cache[0], cache, batch)
+
+
+def test_a_workspace_of_an_unknown_type_is_a_type_error():
+    with pytest.raises(TypeError):
+        A.spconv_attention_workspace(torch.float64, host_batch(), 8, 2, 64)
+    assert A.spconv_attention_workspace(torch.float16, host_batch(), 8, 2, 64) == 0
