@@ -16,6 +16,7 @@ from __future__ import annotations
 import ctypes
 from contextlib import contextmanager
 from functools import lru_cache
+from operator import index
 
 import numpy as np
 import torch
@@ -190,6 +191,8 @@ class CacheBatch:
         if table.dtype is not torch.int32 or table.dim() != 2 or (table.shape[1] > 1 and table.stride(1) != 1):
             raise TypeError("table must be an int32 [sequences, blocks] tensor with contiguous rows")
         B, nb = table.shape
+        block, q_block = index(block), index(q_block)  # (an equal float would find what is remembered for the number)
+        tokens = None if tokens is None else index(tokens)
         stride = table.stride(0) if B > 1 else nb
         _whole(kv_len, "kv_len", torch.int32, (B,), self.device)
         if q_start is not None:
@@ -352,6 +355,7 @@ def spconv_attention_workspace(dtype, batch: CacheBatch, q_heads: int, heads: in
     """Bytes of scratch memory of a ``spconv_block_attention`` call of these sizes."""
     if dtype not in _DTYPES:
         raise TypeError(f"dtype must be float32, float16 or bfloat16, not {dtype}")
+    q_heads, heads, dim, keep = index(q_heads), index(heads), index(dim), index(keep)  # (equal floats are remembered sizes, too)
     return _workspace(_DTYPES[dtype], batch.sequences, batch.block, batch.max_blocks, batch.q_block, batch.tokens,
                       batch.q_start is None, q_heads, heads, dim, keep)
 

@@ -61,3 +61,18 @@ def test_a_workspace_of_an_unknown_type_is_a_type_error():
     with pytest.raises(TypeError):
         A.spconv_attention_workspace(torch.float64, host_batch(), 8, 2, 64)
     assert A.spconv_attention_workspace(torch.float16, host_batch(), 8, 2, 64) == 0
+
+
+def test_sizes_are_whole_numbers(monkeypatch):
+    """Also where the library's answer for the equal number is remembered."""
+    monkeypatch.setattr(A, "_device", lambda t, name: t.device)
+    table, kv, start = torch.zeros((2, 4), dtype=torch.int32), torch.ones(2, dtype=torch.int32), torch.zeros(3, dtype=torch.int32)
+    assert A.CacheBatch(table, kv, 16, start, 40, 8).rows == 40 // 8 + 2
+    for bad in [dict(block=16.0), dict(q_block=8.0), dict(tokens=40.0)]:
+        with pytest.raises(TypeError):
+            A.CacheBatch(table, kv, **{**dict(block=16, q_start=start, tokens=40, q_block=8), **bad})
+    args = dict(q_heads=8, heads=2, dim=64, keep=4)
+    A.spconv_attention_workspace(torch.float16, host_batch(), **args)
+    for name in args:
+        with pytest.raises(TypeError):
+            A.spconv_attention_workspace(torch.float16, host_batch(), **{**args, name: float(args[name])})
