@@ -271,13 +271,18 @@ __global__ __launch_bounds__(ONE ? 256 : 512, NK <= 4 ? 4 : 2) void scores_kerne
                 if (lane < 16 && j < B.max_blocks) out[j] = -kInf;
             }
     }
-    // Again in fp32.
+    // Again in fp32, by the mean keys: a product with the sum may pass the range where that with the mean does not.
     for (int i = 0; again != 0; ++i, again >>= 1) {
         if (!(again & 1)) continue;
         fetch(i);
         int key0[4];
         float inv[4], best[4] = {-kInf, -kInf, -kInf, -kInf};
         bounds(i, key0, inv);
+        const float keys = (float)clamp_int(r.kv - (c_base + (i * kWaves + wave) * 16 + col) * B.block, 1, B.block);
+#pragma unroll
+        for (int k = 0; k < NK; ++k)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) raw[k].v[e] /= keys;
         for (int m0 = 0; m0 < pairs; m0 += 16) {
             const int m = m0 + col;
             const int p = m < pairs ? r.p0 + (int)((uint32_t)m / a.group_div) : -1;
@@ -290,7 +295,7 @@ __global__ __launch_bounds__(ONE ? 256 : 512, NK <= 4 ? 4 : 2) void scores_kerne
             }
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                if (p >= key0[e]) best[e] = fmaxf(best[e], acc[e] * inv[e]);
+                if (p >= key0[e]) best[e] = fmaxf(best[e], acc[e]);
         }
         finish(i, best);
     }

@@ -166,3 +166,19 @@ def test_a_rotation_of_what_requires_grad_is_refused():
         A.spconv_rope(x, *args)
     with torch.no_grad():
         assert torch.equal(A.spconv_rope(x, *args), A.spconv_rope(x.detach(), *args))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("q_block", [1, 16])
+def test_scores_of_sums_near_the_top_of_the_range(dtype, q_block):
+    """Scores are products with the mean key: one that is finite comes out, also where that with the sum is not."""
+    rng = np.random.default_rng(81 + q_block)
+    s = Setup(rng, [20], [500], 64, 2, 64, dtype, q_block)
+    sums = normal(rng, (s.pages, 2, 64), torch.float32)
+    sums[int(s.table[0, 2])] *= 5e37
+    sums[int(s.table[0, 4]), 1, 3] = 3.4e38
+    sums[int(s.table[0, 7]), 0] *= 1e37  # a block of 52 keys
+    q = normal(rng, (20, 8, 64), dtype)
+    want, bound = O.scores(s.rows, f64(q), f64(sums), s.table, s.kv, 64, 2)
+    assert np.abs(want[np.isfinite(want)]).max() < 2.0 ** 127
+    near(A.spconv_block_scores(q, sums, s.batch), want, bound)
