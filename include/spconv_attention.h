@@ -213,8 +213,8 @@ int spconv_attention_workspace(int dtype, const spconv_batch *batch, int q_heads
  *          call) need workspaces of their own.
  * Results are reproducible run to run for a given device and sizes.
  * Errors: SPCONV_EINVAL (NULL pointer, bad batch, unknown dtype, q_heads not a multiple of heads or above 65535,
- * dim not a multiple of 8 in [8, 256], a negative stride, a scale that is not finite, keep < 0, blocks without keep or keep without
- * blocks, counts without blocks, out == q, 2^27 tiles or more of 16 to 256 (token, head) pairs of a row, a workspace
+ * dim not a multiple of 8 in [8, 256], a negative stride, a scale whose product with log2(e) is not finite, keep < 0,
+ * blocks without keep or keep without blocks, counts without blocks, out == q, 2^27 tiles or more of 16 to 256 (token, head) pairs of a row, a workspace
  * that is too small or misaligned); SPCONV_EHIP.
  */
 int spconv_block_attention(int dtype, const spconv_batch *batch, const void *q, int64_t q_token, int64_t q_head,

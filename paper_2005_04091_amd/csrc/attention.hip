@@ -1282,7 +1282,7 @@ extern "C" int spconv_block_attention(int dtype, const spconv_batch *batch, cons
     if (!batch_ok(batch) || !batch_arrays_ok(batch) || !dtype_ok(dtype) || !heads_ok(q_heads, heads, dim) ||
         q == nullptr || k_cache == nullptr || v_cache == nullptr || out == nullptr || q_token < 0 || q_head < 0 ||
         !out_strides_ok(batch->tokens, q_heads, dim, out_token, out_head) || !aligned16(k_cache) ||
-        !aligned16(v_cache) || !std::isfinite(scale) || keep < 0 || (blocks == nullptr) != (keep == 0) ||
+        !aligned16(v_cache) || !std::isfinite(scale * kLog2e) || keep < 0 || (blocks == nullptr) != (keep == 0) ||
         (counts != nullptr && blocks == nullptr) || out == q || !plan_of(dtype, batch, q_heads, heads, dim, keep, &p))
         return SPCONV_EINVAL;
     if (p.bytes > 0 && (workspace == nullptr || !aligned16(workspace) || workspace_bytes < p.bytes)) return SPCONV_EINVAL;

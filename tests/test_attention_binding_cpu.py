@@ -1,9 +1,11 @@
-"""What the binding of the attention calls refuses before the library is asked. No GPU: host tensors stand for device ones, and
-nothing is queued."""
+"""What the attention calls refuse: the binding before the library is asked, and the library. No GPU: host tensors stand for
+device ones, and nothing is queued."""
 import pytest
 import torch
 
 from paper_2005_04091_amd import attention as A
+
+P = 4096  # an aligned address; nothing is read there
 
 
 def host_batch(B=3, nb=4, block=16, q_block=1):
@@ -76,3 +78,12 @@ def test_sizes_are_whole_numbers(monkeypatch):
     for name in args:
         with pytest.raises(TypeError):
             A.spconv_attention_workspace(torch.float16, host_batch(), **{**args, name: float(args[name])})
+
+
+def test_a_scale_past_the_range_is_refused():
+    """The kernels count in powers of two: a scale whose product with log2(e) is infinite would make every output NaN."""
+    def attend(scale):
+        return A._lib.spconv_block_attention(2, A.spconv_batch(2, 64, 8, 1, 10, 20, 8, P, P, P), P, 4096, 128, 32, 8, 128, P, P, scale, P, P,
+                                             4, P + 64, 4096, 128, None, P, 1 << 40, None)
+    for scale in (3e38, -3e38, float("inf"), float("nan")):
+        assert attend(scale) == A.SPCONV_EINVAL
