@@ -113,12 +113,11 @@ __device__ __forceinline__ Seq find_seq(const spconv_batch &B, int x, int div, i
     Seq s;
     const int tokens = (int)B.tokens;
     x = uniform(x);
-    if (B.q_start == nullptr) {  // one item each
-        s.b = x < B.sequences ? x : -1;
+    if (B.q_start == nullptr) {  // (x is a sequence: one item each)
+        s.b = x;
         s.first = x;
-        s.n = s.b < 0 ? 0 : 1;
-        s.at = s.kv = 0;
-        if (s.b < 0) return s;
+        s.n = 1;
+        s.at = 0;
     } else {
         const int lane = threadIdx.x & (kWave - 1);
         s.b = 0;
@@ -154,8 +153,10 @@ struct Row {
 
 __device__ __forceinline__ Row find_row(const spconv_batch &B, int row) {
     if (B.q_start == nullptr) {
-        const Seq s = find_seq(B, sequence_of_row(uniform(row), B.q_block, B.sequences), 1, 0);
-        return {s.b, s.first, s.n, s.kv - 1, s.kv};
+        const int b = sequence_of_row(uniform(row), B.q_block, B.sequences);
+        if (b < 0) return {-1, 0, 0, 0, 0};
+        const Seq s = find_seq(B, b, 1, 0);
+        return {b, b, 1, s.kv - 1, s.kv};
     }
     const Seq s = B.q_block == 1 ? find_seq(B, row, 1, 0) : find_seq(B, row, B.q_block, 1);
     Row r{s.b, 0, 0, 0, s.kv};
