@@ -22,9 +22,10 @@
  *
  * Element types (dtype): keys, values, queries and outputs of one call have the
  * same type. Dot products, softmax statistics, sums, scores and partial outputs
- * are fp32, angles fp64 (their sines and cosines fp32); a value is rounded to its type once, when it is stored
- * (fp16 and bf16 attention rounds the softmax weights to the type as well, for
- * the matrix cores).
+ * are fp32, angles fp64 (their sines and cosines fp32); a value is rounded to its
+ * type once, when it is stored. fp16 and bf16 attention rounds the softmax weights
+ * to the type as well, for the matrix cores: half a step of the type for each
+ * weight, on top of the output's own.
  */
 #ifndef SPCONV_ATTENTION_H
 #define SPCONV_ATTENTION_H
@@ -44,7 +45,7 @@ extern "C" {
 
 /* Flags of spconv_rope and spconv_cache_append. Any other bit is SPCONV_EINVAL. */
 #define SPCONV_ROPE_INTERLEAVED 1u /* pairs (2i, 2i+1); without it pairs (i, i + rot/2) */
-#define SPCONV_ROPE_INVERSE 2u     /* angle -> -angle: undoes the rotation, and is its gradient (spconv_rope only) */
+#define SPCONV_ROPE_INVERSE 2u     /* angle -> -angle: the gradient with the same amplitude, undoes the rotation with 1 / amplitude (spconv_rope only) */
 
 /*
  * The sequences of a step: where their tokens, keys and rows are.
@@ -119,12 +120,13 @@ int spconv_rope_frequencies(int rot, double base, const spconv_rope_scaling *sca
  * components from rot on are copied.
  * x, out     device; token t, head h, component d at t*token_stride + h*head_stride + d
  *            (elements). out may be x itself with x's strides (in place); otherwise they must
- *            not overlap. Vectors are used where pointers and strides are 16-byte multiples.
+ *            not overlap, nor any two rows of out (strides below dim are refused). Moved by the widest vectors,
+ *            16 bytes to one element, that dim, rot, pointers and strides fit.
  * positions  device int32 [tokens], any value.   freq  device fp64 [rot/2].
  * dim        1 to 1024; rot even, 0 to dim (freq may be NULL with rot 0).
  * Errors: SPCONV_EINVAL (NULL pointer, unknown dtype or flags, tokens outside [1, 2^31-1],
- * heads outside [1, 65535], dim or rot out of range, a negative stride, an amplitude that is not finite, x == out
- * with other strides); SPCONV_EHIP when the launch fails.
+ * heads outside [1, 65535], dim or rot out of range, a negative stride, a stride of out below dim, an amplitude that is
+ * not finite, x == out with other strides); SPCONV_EHIP when the launch fails.
  */
 int spconv_rope(int dtype, const void *x, int64_t x_token, int64_t x_head, int64_t tokens, int heads, int dim,
                 const int32_t *positions, const double *freq, int rot, uint32_t flags, float amplitude, void *out,
@@ -140,7 +142,8 @@ int spconv_rope(int dtype, const void *x, int64_t x_token, int64_t x_head, int64
  * earlier position, after drafted tokens were dropped, leaves no trace of them.
  * A page that gets keys must belong to one sequence of the batch (pages that are only
  * read may be shared); the slots of two sequences in one page are otherwise stored in an unspecified order.
- * k, v       device, [tokens][heads][dim] by strides as in spconv_rope.
+ * k, v       device, [tokens][heads][dim] by strides as in spconv_rope. Moved by 16-byte vectors where dim, rot and
+ *            both tensors' pointers and strides fit, otherwise one by one.
  * k_cache, v_cache  device [pages][heads][block][dim], 16-byte aligned.
  * sums       device fp32 [pages][heads][dim], 16-byte aligned, nullable. None of the outputs may overlap the inputs.
  * positions  device int32 [tokens], nullable.  freq  device fp64 [rot/2], nullable (no rotation; rot must be 0).
@@ -164,8 +167,8 @@ int spconv_cache_append(int dtype, const spconv_batch *batch, const void *k, int
  * sums     device fp32 [pages][heads][dim], 16-byte aligned, as spconv_cache_append keeps them.
  * scores   device fp32 [R][heads][max_blocks]; every element is written, must not overlap the inputs.
  * Errors: SPCONV_EINVAL (NULL pointer, bad batch, unknown dtype, q_heads not a multiple of heads or
- * above 65535, dim not a multiple of 8 in [8, 256], R*heads*ceil(max_blocks/64) >= 2^31, a negative stride);
- * SPCONV_EHIP.
+ * above 65535, dim not a multiple of 8 in [8, 256], R*heads*ceil(max_blocks/n) >= 2^31 with n = 64 for rows of 16
+ * (token, query head) pairs or less and 256 for others, a negative stride); SPCONV_EHIP.
  */
 int spconv_block_scores(int dtype, const spconv_batch *batch, const void *q, int64_t q_token, int64_t q_head,
                         int q_heads, int heads, int dim, const float *sums, float *scores, hipStream_t stream);
@@ -200,13 +203,16 @@ int spconv_attention_workspace(int dtype, const spconv_batch *batch, int q_heads
  *   out = sum over S of w_j v_j,  w_j = exp(scale * q.k_j) / sum over S of exp(scale * q.k_i)
  *   lse = log of that sum
  * A token that sees no key gets out = 0 and lse = -infinity (one whose every scale * q.k is -infinity as well).
- * Keys that a token does not see take no part whatever they hold (infinities and NaN among it).
+ * Keys that a token does not see take no part whatever they hold (infinities and NaN among it). Infinities and NaN of
+ * keys that it sees come out by the formula, except that an infinite value whose weight is rounded to 0 (by less
+ * than 2^-25 of the largest in fp16, 2^-126 in the others) may give NaN.
  * blocks   device int32 [R][heads][keep], any order; entries outside [0, max_blocks) and blocks without a page
  *          are passed over, a block that is listed twice counts twice. NULL (with keep 0 and counts NULL): every
  *          visible block (what batch->q_block says is then of no matter).
  * counts   device int32 [R][heads], nullable (then all keep entries are looked at); taken into [0, keep].
  * k_cache, v_cache  device [pages][heads][block][dim], 16-byte aligned.
- * out      device, [tokens][q_heads][dim] by strides, must not overlap the inputs.
+ * out      device, [tokens][q_heads][dim] by strides, must not overlap the inputs, nor its rows each other (strides
+ *          below dim are refused).
  * lse      device fp32 [tokens][q_heads], nullable.
  * workspace  device, 16-byte aligned, at least spconv_attention_workspace bytes (nullable if that is 0); its
  *          contents do not matter. Calls that may run at the same time (other streams, graphs that hold the

@@ -259,7 +259,8 @@ def _freq(freq, device):
 def spconv_rope(x, positions, freq, interleaved: bool = False, inverse: bool = False, amplitude: float = 1.0, out=None,
                 stream=None):
     """``x`` [tokens, heads, dim] rotated by ``positions`` (int32 [tokens]) in its first 2*len(``freq``) components.
-    ``inverse`` undoes it (and is its gradient, with the same amplitude). ``out`` may be ``x``."""
+    ``inverse`` turns back: with the same ``amplitude`` it is the gradient, with 1 / ``amplitude`` it undoes the rotation.
+    ``out`` may be ``x``."""
     device = _device(x, "x")
     T, H, D = _dims(x, "x", _QUERIES)
     code = _dtype(x, "x")

@@ -409,6 +409,9 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && NC <= 4 ? 2 : 1) void rows_k
             for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
+                    // (fp16 and bf16: rounded for the matrix unit, half a step each. The sum is that of the weights before it:
+                    // each wave's largest is exactly 1, so that no rounding of a weight that outweighs the others is left to
+                    // cancel, as there is in the tiles below.)
                     const float p = __builtin_amdgcn_exp2f(x[t][i] - ref);
                     total += p;
                     w[t * 4 + i] = (T)p;
@@ -1160,7 +1163,7 @@ bool plan_of(int dtype, const spconv_batch *B, int q_heads, int heads, int dim, 
     p->batch = *B;
     // Without lists rows mean nothing to the result: they are as long as a tile has room for, and sequences tokens.
     // (Two sequences, 1000 tokens, 4 heads of 4 queries and 128 components, rows of one token given: 549 -> 66 us.)
-    if (keep == 0 && !B->q_start) p->batch.q_block = 1;
+    if (keep == 0 && !B->q_start) p->batch.q_block = 1;  // (then no row is empty)
     if (keep == 0 && B->q_start) {
         const int64_t tokens = (B->tokens + B->sequences - 1) / B->sequences;
         int q = std::min(std::max(most * 32 / group, 1), 128);
